@@ -402,6 +402,153 @@ tq_status tq_search_noalloc(const tq_index *idx, const float *Q_dev, int64_t nq,
  * (0 after any other path). */
 int32_t tq_last_search_fallbacks(void);
 
+/* -------------------------------------------- a language model's reader ---
+ * The passages that a search returns are read by a language model.  The calls
+ * below are that reader's side on the same GPU: attention over whole prompts,
+ * a cache of keys and values in 8-bit codes held in pages, attention over
+ * that cache, and the pages' bookkeeping on the device.  None of them
+ * synchronises, copies to the host or allocates device memory; all can be
+ * captured into a HIP graph.
+ *
+ * The cache.  A page holds 64 consecutive tokens of one row (one sequence);
+ * a scale covers 16 tokens of one head (a block):
+ *   k_dev        [layers][pages][kv_heads][64][head_dim]      codes
+ *   v_dev        [layers][pages][kv_heads][4][head_dim][16]   codes, the
+ *                tokens of a block innermost
+ *   k_scale_dev, v_scale_dev  [layers][pages][kv_heads][4]    float32
+ * A code z of a block with scale s stands for s * z.  TQ_KV_INT8 codes are
+ * int8 in [-127, 127], TQ_KV_FP8 codes OCP e4m3 up to +-448.
+ * 16-byte alignment of k_dev and v_dev.  status_dev (one int32, may be NULL)
+ * collects TQ_KV_* condition bits, which the kernels only ever set: the
+ * caller clears and reads it when it suits.
+ *
+ * Rows.  tables_dev [rows][width] int32 names the pages of each row in order
+ * (-1: none); lens_dev [rows] int32 is its length in tokens, INCLUDING the
+ * tokens that a call appends or that hold its queries; starts_dev [rows + 1]
+ * int32 (0 first, ascending, the number of new tokens last) says which of the
+ * call's packed new tokens are whose.  NULL starts_dev: one new token per
+ * row.  The i-th of a row's n new tokens has position len - n + i.
+ * Values that lie on the device are not checked by the host: a page id outside [0, pages) is
+ * skipped (TQ_KV_BAD_PAGE), a length beyond width pages is cut, tokens
+ * outside the packed tensor are left out. */
+typedef enum { TQ_KV_INT8 = 0, TQ_KV_FP8 = 1 } tq_kv_type;
+typedef enum { TQ_F16 = 0, TQ_BF16 = 1 } tq_float;
+#define TQ_KV_PAGE 64
+#define TQ_KV_BLOCK 16
+/* bits of the status word */
+#define TQ_KV_NONFINITE 1   /* an appended value was infinite or not a number */
+#define TQ_KV_BAD_PAGE 2    /* a page id outside the pool was named */
+#define TQ_KV_FULL 4        /* a row did not get the pages it asked for */
+
+typedef struct {
+    void *k_dev, *v_dev;
+    float *k_scale_dev, *v_scale_dev;
+    int32_t *status_dev;
+    int64_t pages;
+    int32_t layers, kv_heads, head_dim, type;
+} tq_kv_cache;
+
+/* Packed rows of float16 or bfloat16 vectors: element (token, head, j) at
+ * data_dev[token * token_stride + head * head_stride + j] (strides in
+ * elements, at least 0; the last dimension is contiguous). */
+typedef struct {
+    const void *data_dev;
+    int64_t token_stride, head_stride;
+} tq_rows;
+
+/* Appends new tokens to one layer.  k and v: packed rows [n][kv_heads][head_dim]
+ * of `dtype`.  For each block of 16 positions that receives tokens, and each
+ * head, with c tokens of the block there before:
+ *   a  = largest finite |x| of the block's new values (below 2^-100: 0)
+ *   s1 = max(s0, fl(a * fl(1/qmax))), s0 the block's scale (0 if c = 0),
+ *        qmax 127 or 448
+ *   new codes = round(clamp(fl(x * fl(1/s1)))), ties to even; NaN gives 0
+ *   if s1 > s0, the codes that were there become round(fl(z * fl(s0/s1)))
+ * all in float32.  With c = 0 the block's remaining codes become 0.  Two rows
+ * must not append to the same page.  Errors: TQ_EINVAL for null pointers,
+ * negative sizes or a layer out of range; TQ_EUNSUPPORTED for a head_dim
+ * other than 64, 128, 256. */
+tq_status tq_kv_append(const tq_kv_cache *cache, int32_t layer, const tq_rows *k,
+                       const tq_rows *v, int32_t dtype, int64_t n,
+                       const int32_t *tables_dev, int32_t width,
+                       const int32_t *lens_dev, const int32_t *starts_dev,
+                       int32_t rows, void *stream);
+
+/* Attention of new tokens' queries over the cache of one layer: q packed rows
+ * [n][heads][head_dim] of `dtype`, heads a multiple of kv_heads (consecutive
+ * query heads share a key head).  A query at position p of its row sees the
+ * tokens 0..p:
+ *   out = sum_t w_t v_t / sum_t w_t, w_t = exp(scale * q.k_t),
+ * out_dev [n][heads][head_dim] of `dtype`, contiguous, and, unless NULL, lse_dev [n][heads]
+ * float32 = log sum_t w_t.  A query that sees no token gives 0 and -inf.
+ * `longest` bounds lens_dev (0: width pages); a longer row is cut there.
+ * Statistics and sums are float32; the weights are rounded to float16.
+ * The workspace (tq_kv_attend_workspace bytes, 256-byte aligned) holds the
+ * partial results of long rows, which are split among workgroups. */
+tq_status tq_kv_attend_workspace(const tq_kv_cache *cache, int64_t n, int32_t heads,
+                                 int32_t width, int32_t rows, int32_t longest,
+                                 size_t *bytes_out);
+tq_status tq_kv_attend(const tq_kv_cache *cache, int32_t layer, const tq_rows *q,
+                       int32_t dtype, int64_t n, int32_t heads,
+                       const int32_t *tables_dev, int32_t width,
+                       const int32_t *lens_dev, const int32_t *starts_dev,
+                       int32_t rows, int32_t longest, float scale, void *out_dev,
+                       float *lse_dev, void *workspace_dev,
+                       size_t workspace_bytes, void *stream);
+
+/* The rows' pages.  refs_dev [pages] int32 counts the rows that hold a page
+ * (0: free).  The calls change tables, lens and refs (and copy pages in all
+ * layers of the cache) on the device. */
+typedef struct {
+    int32_t *tables_dev, *lens_dev, *refs_dev;
+    int64_t pages;
+    int32_t rows, width;
+} tq_kv_rows;
+
+/* Workspace of the three calls below, in bytes (n: pairs of tq_kv_fork). */
+tq_status tq_kv_rows_workspace(const tq_kv_rows *rows, int64_t n, size_t *bytes_out);
+
+/* Sets each row's length to goals_dev [rows] int32 (negative: leave it).
+ * First the rows that shrink give back the pages past their new end; then
+ * the rows that grow, in row order, take the lowest free pages, and a row
+ * that grows out of a part-filled page which other rows hold too takes a
+ * copy of that page first.  A row that asks for more pages than are left, or
+ * than `width`, stays as it is (TQ_KV_FULL). */
+tq_status tq_kv_resize(const tq_kv_rows *rows, const int32_t *goals_dev,
+                       const tq_kv_cache *cache, void *workspace_dev,
+                       size_t workspace_bytes, void *stream);
+
+/* Makes row dst_dev[i] a copy of row src_dev[i] (n pairs of row numbers on the
+ * device, dst distinct; a pair of equal rows changes nothing).  All sources
+ * are as they were before the call.  What dst held is given back, whole pages
+ * are shared, and a part-filled last page is copied to the lowest free page
+ * (pages that were free before the call, in the order of i).  Without a page
+ * left the row becomes empty (TQ_KV_FULL). */
+tq_status tq_kv_fork(const tq_kv_rows *rows, const int32_t *src_dev,
+                     const int32_t *dst_dev, int64_t n, const tq_kv_cache *cache,
+                     void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* Moves the live pages to the front of the pool: with L live pages, the i-th
+ * live page from L on goes to the i-th free one below L; tables and refs
+ * follow.  live_dev [1] int32 receives L. */
+tq_status tq_kv_compact(const tq_kv_rows *rows, const tq_kv_cache *cache,
+                        int32_t *live_dev, void *workspace_dev,
+                        size_t workspace_bytes, void *stream);
+
+/* Attention over whole prompts: q packed rows [n][heads][head_dim], k and v
+ * packed rows [n_keys][kv_heads][head_dim], all of `dtype`; starts_dev and
+ * key_starts_dev [rows + 1] (NULL: as starts_dev).  causal: query i of a row
+ * of m queries and l keys sees the keys 0..i + l - m, else all l.  out and
+ * lse as in tq_kv_attend.  head_dim 64, 128 or 256.  `longest` bounds the
+ * queries of a row (0: n).  float32 sums and statistics; the weights are
+ * rounded to `dtype`. */
+tq_status tq_attention(const tq_rows *q, const tq_rows *k, const tq_rows *v,
+                       int32_t dtype, int64_t n, int64_t n_keys, int32_t heads,
+                       int32_t kv_heads, int32_t head_dim,
+                       const int32_t *starts_dev, const int32_t *key_starts_dev,
+                       int32_t rows, int32_t longest, int32_t causal,
+                       float scale, void *out_dev, float *lse_dev, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -8,6 +8,18 @@ the current stream; every step of the method runs in the HIP library.
     idx = Index(cb, rot, n_tenants=1)
     idx.add(X)                                 # X: cuda float32 [n, d]
     ids, scores = idx.search(Q, k=10)          # Q: cuda float32 [nq, d]
+
+A language model's reader next to the index (the passages that a search
+returns go through it): attention over packed prompts, a paged cache of 8-bit
+keys and values, attention over that cache, and the pages' bookkeeping:
+
+    out = attention(q, k, v, starts)           # packed rows, causal
+    cache = KVCache(layers, pages, kv_heads, head_dim, "int8")
+    pages = KVPages(rows, width, pages)
+    pages.resize(goals, cache)                 # lengths of the rows, pages taken or given back
+    cache.append(layer, k, v, pages.tables, pages.lens, starts)
+    out = cache.attend(layer, q, pages.tables, pages.lens, starts)
+    pages.fork(src, dst, cache)                # rows that continue others
 """
 from __future__ import annotations
 
@@ -20,7 +32,7 @@ from ._lib import (AUTO_FILTERED_QUERIES, FLAG_PREROTATED, FLAG_SLOT_ALLOW, PATH
                    lib)
 
 __all__ = ["Codebook", "Rotation", "Index", "IdMapIndex", "TQError", "rotate_quantize",
-           "rotate_queries", "version", "last_search_fallbacks"]
+           "rotate_queries", "version", "last_search_fallbacks", "KVCache", "KVPages", "attention"]
 
 
 def version() -> str:
@@ -439,3 +451,11 @@ class IdMapIndex(Index):
         check(lib.tq_index_remove_ids(self._h, ids.ctypes.data_as(ctypes.c_void_p), ids.shape[0],
                                       ctypes.byref(r)))
         return r.value
+
+
+def __getattr__(name):
+    # the reader's classes need torch at import; the index does not
+    if name in ("KVCache", "KVPages", "attention"):
+        from . import kv
+        return getattr(kv, name)
+    raise AttributeError("module %r has no attribute %r" % (__name__, name))

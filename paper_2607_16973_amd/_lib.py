@@ -23,6 +23,28 @@ AUTO_FILTERED_QUERIES = 6   # TQ_AUTO_FILTERED_QUERIES
 _STATUS = {TQ_EINVAL: "TQ_EINVAL", TQ_ENOMEM: "TQ_ENOMEM", TQ_EDEVICE: "TQ_EDEVICE",
            TQ_EUNSUPPORTED: "TQ_EUNSUPPORTED"}
 
+KV_TYPES = {"int8": 0, "fp8": 1}
+KV_PAGE, KV_BLOCK = 64, 16                    # TQ_KV_PAGE, TQ_KV_BLOCK
+KV_NONFINITE, KV_BAD_PAGE, KV_FULL = 1, 2, 4  # bits of a cache's status
+
+
+class KVCacheView(ctypes.Structure):   # tq_kv_cache
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("status", ctypes.c_void_p),
+                ("pages", ctypes.c_int64), ("layers", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("type", ctypes.c_int32)]
+
+
+class RowsView(ctypes.Structure):      # tq_rows
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
+class KVRowsView(ctypes.Structure):    # tq_kv_rows
+    _fields_ = [("tables", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("refs", ctypes.c_void_p),
+                ("pages", ctypes.c_int64), ("rows", ctypes.c_int32), ("width", ctypes.c_int32)]
+
 
 class TQError(RuntimeError):
     def __init__(self, status: int, message: str):
@@ -75,6 +97,16 @@ def _load():
         "tq_search_ex": ([P, P, I64, I32, P, I32, P, SZ, P, P, P], ctypes.c_int),
         "tq_search_noalloc": ([P, P, I64, I32, P, P, P, P], ctypes.c_int),
         "tq_last_search_fallbacks": ([], ctypes.c_int32),
+        "tq_kv_append": ([P, I32, P, P, I32, I64, P, I32, P, P, I32, P], ctypes.c_int),
+        "tq_kv_attend_workspace": ([P, I64, I32, I32, I32, I32, P], ctypes.c_int),
+        "tq_kv_attend": ([P, I32, P, I32, I64, I32, P, I32, P, P, I32, I32, ctypes.c_float, P, P,
+                          P, SZ, P], ctypes.c_int),
+        "tq_kv_rows_workspace": ([P, I64, P], ctypes.c_int),
+        "tq_kv_resize": ([P, P, P, P, SZ, P], ctypes.c_int),
+        "tq_kv_fork": ([P, P, P, I64, P, P, SZ, P], ctypes.c_int),
+        "tq_kv_compact": ([P, P, P, P, SZ, P], ctypes.c_int),
+        "tq_attention": ([P, P, P, I32, I64, I64, I32, I32, I32, P, P, I32, I32, I32,
+                          ctypes.c_float, P, P, P], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         f = getattr(lib, name)
@@ -93,7 +125,9 @@ EXPORTED = ("tq_last_error", "tq_version", "tq_build_codebook", "tq_codebook_tab
             "tq_index_slots", "tq_slot_allowlist", "tq_index_calibrate",
             "tq_index_set_calibration", "tq_index_calibration",
             "tq_index_free", "tq_search", "tq_search_postfilter", "tq_search_workspace_size",
-            "tq_search_ex", "tq_search_noalloc", "tq_last_search_fallbacks")
+            "tq_search_ex", "tq_search_noalloc", "tq_last_search_fallbacks", "tq_kv_append",
+            "tq_kv_attend_workspace", "tq_kv_attend", "tq_kv_rows_workspace", "tq_kv_resize",
+            "tq_kv_fork", "tq_kv_compact", "tq_attention")
 
 
 def check(status: int) -> None:

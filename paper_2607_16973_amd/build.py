@@ -22,7 +22,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libtq.so")
 
 HIP_SOURCES = ["encode.hip", "scan.hip", "batch.hip", "layout.hip", "calib.hip", "noalloc.hip",
-               "api.cpp"]
+               "attention.hip", "kv_append.hip", "kv_attend.hip", "kv_pages.hip", "api.cpp",
+               "kv_api.cpp"]
 # Per-source extra flags.  The scan's prefetch ring must stay where it is
 # written: machine sinking would move every refill into the loop latch and
 # serialise the loads with the table lookups (in the encode GEMM it moves

@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "kernels.h"
+#include "status.h"
 #include "tq_internal.h"
 
 namespace tq {
@@ -40,6 +41,8 @@ tq_status check_geometry(int32_t d, int32_t bits) {
     return TQ_OK;
 }
 
+}  // namespace
+
 tq_status device_ready() {
     int n = 0;
     hipError_t e = hipGetDeviceCount(&n);
@@ -57,6 +60,8 @@ tq_status hip_fail(hipError_t e, const char *what) {
         return fail(TQ_ENOMEM, std::string(what) + ": out of device memory");
     return fail(TQ_EDEVICE, std::string(what) + ": " + hipGetErrorString(e));
 }
+
+namespace {
 
 void fill_codebook_dev(const CodebookTables &t, CodebookDev *cd) {
     std::memset(cd, 0, sizeof(*cd));

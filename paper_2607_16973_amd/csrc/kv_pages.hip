@@ -1,0 +1,401 @@
+// The pages of the cache's rows: resize, fork, compact, all on the device.
+//
+// Every choice (which free page goes to whom) is an exclusive prefix sum over
+// rows or page ids, so results do not depend on timing: one workgroup makes
+// it (kv_*_plan), then grids apply it to the tables and copy pages in all
+// layers.  The counters in refs are integers, so the order of their atomic
+// updates does not show.  Bound by latency (a few launches of a few
+// microseconds) for the tables and by memory for the copies.
+#include <hip/hip_runtime.h>
+
+#include "kv.h"
+
+namespace tq {
+namespace {
+
+constexpr int kPlanThreads = 1024;
+
+// Exclusive prefix sum over the workgroup's threads; *total receives the sum.
+__device__ inline int block_scan(int x, int *lds, int *total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int inc = x;
+    for (int m = 1; m < 64; m <<= 1) {
+        const int y = __shfl_up(inc, m);
+        if (lane >= m) inc += y;
+    }
+    __syncthreads();   // lds may still be read by the call before
+    if (lane == 63) lds[wave] = inc;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < kPlanThreads / 64; ++w) {
+        const int s = lds[w];
+        before += w < wave ? s : 0;
+        all += s;
+    }
+    *total = all;
+    return before + inc - x;
+}
+
+// The ids p with refs[p] == 0 in ascending order into out, until `want` of
+// them are found or the pool ends; returns how many there are (at least min(want, all)).
+__device__ inline int list_free(const int *refs, int pages, int want, int *out, int *lds) {
+    int found = 0;
+    for (int base = 0; base < pages && found < want; base += kPlanThreads * 4) {
+        int id[4], n = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int p = base + threadIdx.x * 4 + j;
+            id[j] = p < pages && refs[p] == 0;
+            n += id[j];
+        }
+        int all;
+        int at = found + block_scan(n, lds, &all);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (id[j] && at < want) out[at++] = base + threadIdx.x * 4 + j;
+        found += all;
+    }
+    return found;
+}
+
+__device__ inline int pages_of(int tokens) { return (tokens + kPage - 1) / kPage; }
+__device__ inline void flag(int *status, int bit) {
+    if (status) atomicOr(status, bit);
+}
+
+// Workspace: ints.
+struct Scratch {
+    int *head;        // [4]: free pages found, pairs to copy, live pages
+    int *begin;       // [n] first of a row's or pair's places in fresh
+    int *more;        // [n] pages it asks for; bit 30: the first one replaces a shared page
+    int *from, *to;   // [m] pairs of pages to copy (from -1: none)
+    int *fresh;       // [pages] free pages taken, in order
+    int *stage;       // [n][width] rows on their way (fork)
+    int *slens;       // [n]
+};
+constexpr int kCopied = 1 << 30;
+
+__host__ __device__ inline Scratch scratch(void *ws, int64_t pages, int64_t rows, int64_t n) {
+    const int64_t m = rows > n ? rows : n, pairs = m > pages ? m : pages;
+    Scratch s;
+    s.head = static_cast<int *>(ws);
+    s.begin = s.head + 4;
+    s.more = s.begin + m;
+    s.from = s.more + m;
+    s.to = s.from + pairs;
+    s.fresh = s.to + pairs;
+    s.slens = s.fresh + pages;
+    s.stage = s.slens + n;
+    return s;
+}
+
+// ------------------------------------------------------------------ copies
+// Copies pages from[i] -> to[i], i < count, in all layers: pieces of 16 KiB
+// of one store (16 bytes x 4 per thread in flight), the scales with the first.
+constexpr int kPiece = 16384;
+__global__ __launch_bounds__(256) void copy_pages_kernel(PagesArgs a, const int *from, const int *to,
+                                                         const int *device_count, int count) {
+    if (device_count) count = min(count, *device_count);
+    const int64_t store = (int64_t)a.cache.heads * kPage * a.D;   // bytes of a page in one store
+    const int pieces = (int)((store + kPiece - 1) / kPiece);
+    const int64_t units = (int64_t)a.layers * count * 2 * pieces;
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+        const int piece = (int)(u % pieces);
+        const int64_t v = u / pieces;
+        const int which = (int)(v & 1);
+        const int64_t w = v >> 1;
+        const int layer = (int)(w / count), i = (int)(w % count);
+        const int src = from[i], dst = to[i];
+        if (src < 0) continue;
+        const int64_t base = (int64_t)layer * a.cache.pages;
+        char *codes = which ? a.cache.v : a.cache.k;
+        const uint4 *s = reinterpret_cast<const uint4 *>(codes + (base + src) * store + (int64_t)piece * kPiece);
+        uint4 *d = reinterpret_cast<uint4 *>(codes + (base + dst) * store + (int64_t)piece * kPiece);
+        const int n = (int)(min(store - (int64_t)piece * kPiece, (int64_t)kPiece) / 16);
+        uint4 x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j * 256 + (int)threadIdx.x < n) x[j] = s[j * 256 + threadIdx.x];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j * 256 + (int)threadIdx.x < n) d[j * 256 + threadIdx.x] = x[j];
+        if (piece == 0) {
+            float *sc = which ? a.cache.vs : a.cache.ks;
+            const int64_t row = (int64_t)a.cache.heads * 4;
+            for (int j = threadIdx.x; j < (int)row; j += 256)
+                sc[(base + dst) * row + j] = sc[(base + src) * row + j];
+        }
+    }
+}
+
+void launch_copy(const PagesArgs &a, const int *from, const int *to, const int *device_count, int count,
+                 hipStream_t stream) {
+    const int64_t store = (int64_t)a.cache.heads * kPage * a.D;
+    const int64_t units = (int64_t)a.layers * count * 2 * ((store + kPiece - 1) / kPiece);
+    const int64_t most = 256 * 8;
+    copy_pages_kernel<<<(unsigned)(units < most ? units : most), 256, 0, stream>>>(a, from, to, device_count, count);
+}
+
+// ------------------------------------------------------------------ resize
+// A wave per row: gives back the pages past a smaller goal.
+__global__ __launch_bounds__(256) void shrink_kernel(PagesArgs a, const int *goals) {
+    const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (row >= a.rows) return;
+    const int len = min(max(a.lens[row], 0), a.width * kPage);
+    const int goal = goals[row];
+    if (goal < 0 || goal >= len) return;
+    for (int col = pages_of(goal) + lane; col < pages_of(len); col += 64) {
+        int *at = &a.tables[(int64_t)row * a.width + col];
+        const int page = *at;
+        if (page >= 0 && page < a.pages) atomicSub(&a.refs[page], 1);
+        else flag(a.cache.status, TQ_KV_BAD_PAGE);
+        *at = -1;
+    }
+    if (lane == 0) a.lens[row] = goal;
+}
+
+// One workgroup: how many pages each growing row asks for and where they
+// begin in the list of free ones; that list.
+__global__ __launch_bounds__(kPlanThreads) void resize_plan_kernel(PagesArgs a, const int *goals) {
+    __shared__ int lds[kPlanThreads / 64];
+    const Scratch s = scratch(a.ws, a.pages, a.rows, 0);
+    int total = 0;
+    for (int base = 0; base < a.rows; base += kPlanThreads) {
+        const int row = base + threadIdx.x;
+        int more = 0;
+        bool shared = false;
+        if (row < a.rows) {
+            const int len = min(max(a.lens[row], 0), a.width * kPage), goal = goals[row];
+            if (goal > len) {
+                if (goal > a.width * kPage) {
+                    flag(a.cache.status, TQ_KV_FULL);
+                } else {
+                    more = pages_of(goal) - pages_of(len);
+                    if (len % kPage) {
+                        const int page = a.tables[(int64_t)row * a.width + len / kPage];
+                        if (page >= 0 && page < a.pages) shared = a.refs[page] > 1;
+                        else flag(a.cache.status, TQ_KV_BAD_PAGE);
+                    }
+                    more += shared;
+                }
+            }
+        }
+        int all;
+        const int at = total + block_scan(more, lds, &all);
+        if (row < a.rows) {
+            s.begin[row] = at;
+            s.more[row] = more | (shared ? kCopied : 0);
+        }
+        total += all;
+    }
+    const int found = list_free(a.refs, a.pages, min(total, a.pages), s.fresh, lds);
+    if (threadIdx.x == 0) s.head[0] = found;
+}
+
+// A wave per row: takes its pages.
+__global__ __launch_bounds__(256) void grow_kernel(PagesArgs a, const int *goals) {
+    const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (row >= a.rows) return;
+    const Scratch s = scratch(a.ws, a.pages, a.rows, 0);
+    if (lane == 0) s.from[row] = -1;
+    const int len = min(max(a.lens[row], 0), a.width * kPage), goal = goals[row];
+    if (goal <= len || goal > a.width * kPage) return;
+    const bool shared = s.more[row] & kCopied;
+    const int more = s.more[row] & ~kCopied, begin = s.begin[row];
+    if (more > 0 && (int64_t)begin + more > s.head[0]) {
+        if (lane == 0) flag(a.cache.status, TQ_KV_FULL);
+        return;
+    }
+    int *table = a.tables + (int64_t)row * a.width;
+    const int first = pages_of(len) - (shared ? 1 : 0);
+    if (shared && lane == 0) {
+        const int old = table[first];
+        atomicSub(&a.refs[old], 1);
+        s.from[row] = old;
+        s.to[row] = s.fresh[begin];
+    }
+    for (int j = lane; j < more; j += 64) {
+        const int page = s.fresh[begin + j];
+        a.refs[page] = 1;
+        table[first + j] = page;
+    }
+    if (lane == 0) a.lens[row] = goal;
+}
+
+// -------------------------------------------------------------------- fork
+__device__ inline bool pair_rows(const PagesArgs &a, const int *src, const int *dst, int i, int *from, int *to) {
+    *from = src[i];
+    *to = dst[i];
+    return *from != *to && *from >= 0 && *from < a.rows && *to >= 0 && *to < a.rows;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(PagesArgs a, const int *src, const int *dst, int n) {
+    __shared__ int lds[kPlanThreads / 64];
+    const Scratch s = scratch(a.ws, a.pages, a.rows, n);
+    int total = 0;
+    for (int base = 0; base < n; base += kPlanThreads) {
+        const int i = base + threadIdx.x;
+        int part = 0, from, to;
+        if (i < n && pair_rows(a, src, dst, i, &from, &to))
+            part = min(max(a.lens[from], 0), a.width * kPage) % kPage != 0;
+        int all;
+        const int at = total + block_scan(part, lds, &all);
+        if (i < n) {
+            s.begin[i] = at;
+            s.more[i] = part;
+        }
+        total += all;
+    }
+    const int found = list_free(a.refs, a.pages, min(total, a.pages), s.fresh, lds);
+    if (threadIdx.x == 0) s.head[0] = found;
+}
+
+// A wave per pair: the new row into the workspace, before any row changes.
+__global__ __launch_bounds__(256) void fork_stage_kernel(PagesArgs a, const int *src, const int *dst, int n) {
+    const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (i >= n) return;
+    const Scratch s = scratch(a.ws, a.pages, a.rows, n);
+    int from, to;
+    if (lane == 0) s.from[i] = -1;
+    if (!pair_rows(a, src, dst, i, &from, &to)) return;
+    const int len = min(max(a.lens[from], 0), a.width * kPage);
+    const bool part = s.more[i], fits = !part || s.begin[i] < s.head[0];
+    const int whole = fits ? len / kPage : 0;
+    const int *table = a.tables + (int64_t)from * a.width;
+    for (int col = lane; col < a.width; col += 64) s.stage[(int64_t)i * a.width + col] = col < whole ? table[col] : -1;
+    if (lane == 0) {
+        s.slens[i] = fits ? len : 0;
+        if (!fits) flag(a.cache.status, TQ_KV_FULL);
+        if (part && fits) {
+            const int old = table[whole], page = s.fresh[s.begin[i]];
+            s.stage[(int64_t)i * a.width + whole] = page;
+            if (old >= 0 && old < a.pages) s.from[i] = old;
+            else flag(a.cache.status, TQ_KV_BAD_PAGE);
+            s.to[i] = page;
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void fork_apply_kernel(PagesArgs a, const int *src, const int *dst, int n) {
+    const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (i >= n) return;
+    const Scratch s = scratch(a.ws, a.pages, a.rows, n);
+    int from, to;
+    if (!pair_rows(a, src, dst, i, &from, &to)) return;
+    int *table = a.tables + (int64_t)to * a.width;
+    for (int col = lane; col < a.width; col += 64) {
+        const int old = table[col], page = s.stage[(int64_t)i * a.width + col];
+        if (old >= 0 && old < a.pages) atomicSub(&a.refs[old], 1);
+        if (page >= 0 && page < a.pages) atomicAdd(&a.refs[page], 1);   // a fresh one: 0 -> 1
+        table[col] = page;
+    }
+    if (lane == 0) a.lens[to] = s.slens[i];
+}
+
+// ----------------------------------------------------------------- compact
+__global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(PagesArgs a, int *live_out) {
+    __shared__ int lds[kPlanThreads / 64];
+    const Scratch s = scratch(a.ws, a.pages, a.rows, 0);
+    int live = 0;
+    for (int base = 0; base < a.pages; base += kPlanThreads * 4) {
+        int n = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int p = base + threadIdx.x * 4 + j;
+            n += p < a.pages && a.refs[p] > 0;
+        }
+        int all;
+        block_scan(n, lds, &all);
+        live += all;
+    }
+    int holes = 0, movers = 0;
+    for (int base = 0; base < a.pages; base += kPlanThreads * 4) {
+        int hole[4], mover[4], nh = 0, nm = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int p = base + threadIdx.x * 4 + j;
+            const bool in = p < a.pages, used = in && a.refs[p] > 0;
+            hole[j] = in && !used && p < live;
+            mover[j] = used && p >= live;
+            nh += hole[j];
+            nm += mover[j];
+        }
+        int all_h, all_m;
+        int ah = holes + block_scan(nh, lds, &all_h);
+        int am = movers + block_scan(nm, lds, &all_m);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int p = base + threadIdx.x * 4 + j;
+            if (hole[j]) s.to[ah++] = p;
+            if (mover[j]) {
+                s.fresh[p] = am;      // which move takes this page
+                s.from[am++] = p;
+            }
+        }
+        holes += all_h;
+        movers += all_m;
+    }
+    if (threadIdx.x == 0) {
+        s.head[1] = movers;           // as many as holes
+        s.head[2] = live;
+        *live_out = live;
+    }
+}
+
+__global__ __launch_bounds__(256) void compact_apply_kernel(PagesArgs a) {
+    const Scratch s = scratch(a.ws, a.pages, a.rows, 0);
+    const int live = s.head[2], moves = s.head[1];
+    const int64_t cells = (int64_t)a.rows * a.width, step = (int64_t)gridDim.x * 256;
+    for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < cells; i += step) {
+        const int page = a.tables[i];
+        if (page >= live && page < a.pages) {
+            const int m = s.fresh[page];
+            // a table may name a page that no count covers: it has no move
+            if (m >= 0 && m < moves && s.from[m] == page) a.tables[i] = s.to[m];
+            else flag(a.cache.status, TQ_KV_BAD_PAGE);
+        }
+    }
+    for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < moves; i += step) {
+        a.refs[s.to[i]] = a.refs[s.from[i]];
+        a.refs[s.from[i]] = 0;
+    }
+}
+
+}  // namespace
+
+size_t kv_rows_bytes(int64_t pages, int64_t rows, int64_t width, int64_t n) {
+    const int64_t m = rows > n ? rows : n, pairs = m > pages ? m : pages;
+    return sizeof(int) * (size_t)(4 + 2 * m + 2 * pairs + pages + n + n * width);
+}
+
+hipError_t kv_resize(const PagesArgs &a, const int *goals, hipStream_t stream) {
+    const unsigned grid = (unsigned)((a.rows + 3) / 4);
+    const Scratch s = scratch(a.ws, a.pages, a.rows, 0);
+    shrink_kernel<<<grid, 256, 0, stream>>>(a, goals);
+    resize_plan_kernel<<<1, kPlanThreads, 0, stream>>>(a, goals);
+    grow_kernel<<<grid, 256, 0, stream>>>(a, goals);
+    launch_copy(a, s.from, s.to, nullptr, a.rows, stream);
+    return hipGetLastError();
+}
+
+hipError_t kv_fork(const PagesArgs &a, const int *src, const int *dst, int n, hipStream_t stream) {
+    const unsigned grid = (unsigned)((n + 3) / 4);
+    const Scratch s = scratch(a.ws, a.pages, a.rows, n);
+    fork_plan_kernel<<<1, kPlanThreads, 0, stream>>>(a, src, dst, n);
+    fork_stage_kernel<<<grid, 256, 0, stream>>>(a, src, dst, n);
+    fork_apply_kernel<<<grid, 256, 0, stream>>>(a, src, dst, n);
+    launch_copy(a, s.from, s.to, nullptr, n, stream);
+    return hipGetLastError();
+}
+
+hipError_t kv_compact(const PagesArgs &a, int *live, hipStream_t stream) {
+    const Scratch s = scratch(a.ws, a.pages, a.rows, 0);
+    const int64_t cells = (int64_t)a.rows * a.width > a.pages ? (int64_t)a.rows * a.width : a.pages;
+    compact_plan_kernel<<<1, kPlanThreads, 0, stream>>>(a, live);
+    const unsigned grid = (unsigned)(cells / 256 + 1 < 1024 ? cells / 256 + 1 : 1024);
+    compact_apply_kernel<<<grid, 256, 0, stream>>>(a);
+    launch_copy(a, s.from, s.to, s.head + 1, a.pages, stream);
+    return hipGetLastError();
+}
+
+}  // namespace tq

@@ -1,0 +1,183 @@
+"""Plain forms of the reader's operators for the tests: attention in float64,
+the cache's quantisation in numpy float32 (its definition, rounding by
+rounding), the pages as Python lists."""
+import math
+
+import numpy as np
+import torch
+
+PAGE, BLOCK = 64, 16
+TOP = {"int8": np.float32(127), "fp8": np.float32(448)}
+
+
+def starts_of(counts, device="cuda"):
+    return torch.tensor([0] + list(np.cumsum(counts)), dtype=torch.int32, device=device)
+
+
+def attention64(q, k, v, pos, scale):
+    """One row, float64: q [n, h, d], k and v [m, hk, d], pos[i] the last key
+    that query i sees.  Returns out, lse and sum_j p_j |v_j| (for bounds)."""
+    q, k, v = q.double().cpu(), k.double().cpu(), v.double().cpu()
+    n, h, d = q.shape
+    g = h // k.shape[1]
+    out, lse = torch.zeros(n, h, d, dtype=torch.float64), torch.full((n, h), -math.inf, dtype=torch.float64)
+    size = torch.zeros_like(out)
+    for i in range(n):
+        m = min(int(pos[i]) + 1, k.shape[0])
+        if m <= 0:
+            continue
+        kk, vv = k[:m].repeat_interleave(g, 1), v[:m].repeat_interleave(g, 1)     # [m, h, d]
+        x = (kk * q[i]).sum(-1) * scale                                            # [m, h]
+        lse[i] = torch.logsumexp(x, 0)
+        p = torch.exp(x - lse[i])[..., None]
+        out[i] = (p * vv).sum(0)
+        size[i] = (p * vv.abs()).sum(0)
+    return out, lse, size
+
+
+def e4m3(x):
+    """float32 array -> nearest e4m3 value (|x| <= 448), ties to even."""
+    x = x.astype(np.float64)
+    e = np.floor(np.log2(np.maximum(np.abs(x), 2.0 ** -6)))
+    step = np.exp2(e - 3)
+    return np.round(x / step) * step
+
+
+def code(x, kind):
+    x = np.where(np.isnan(x), np.float32(0), x)
+    x = np.clip(x, -TOP[kind], TOP[kind])
+    return np.round(x).astype(np.float32) if kind == "int8" else e4m3(x).astype(np.float32)
+
+
+def append_block(z, s0, c, x, kind):
+    """One block of one head: z [16, d] codes, s0 its scale, c tokens there,
+    x [m, d] float32 new ones.  Returns the new codes and scale."""
+    f = np.float32
+    if c == 0:
+        z, s0 = np.zeros_like(z), f(0)
+    fin = np.abs(x)[np.isfinite(x)]
+    a = f(fin.max()) if fin.size else f(0)
+    s1 = max(s0, f(0) if a < f(2.0 ** -100) else f(a * f(f(1) / TOP[kind])))
+    r = f(f(1) / s1) if s1 > 0 else f(0)
+    if c and s1 > s0:
+        z = code(z * f(s0 / s1), kind)
+    z = z.copy()
+    with np.errstate(invalid="ignore", over="ignore"):
+        z[c:c + len(x)] = code((x * r).astype(f), kind)
+    return z, s1
+
+
+class HostCache:
+    """Codes and scales of one layer as numpy float32, tokens in rows."""
+
+    def __init__(self, cache, layer):
+        self.kind = cache.dtype
+        k, v = cache.k[layer].float().cpu().numpy(), cache.v[layer].float().cpu().numpy()
+        p, h, _, d = k.shape
+        self.codes = [k.reshape(p, h, 4, BLOCK, d), np.ascontiguousarray(v.transpose(0, 1, 2, 4, 3))]
+        self.scales = [s[layer].cpu().numpy().copy() for s in (cache.k_scale, cache.v_scale)]
+
+    def append(self, new, table, length):
+        """new: the row's new k and v, [n, h, d] float32; length includes them."""
+        n, at = new[0].shape[0], length - new[0].shape[0]
+        i = 0
+        while i < n:
+            pos = at + i
+            page, sub, c = table[pos // PAGE], pos % PAGE // BLOCK, pos % BLOCK
+            m = min(BLOCK - c, n - i)
+            for which in range(2):
+                for h in range(new[0].shape[1]):
+                    z, s = append_block(self.codes[which][page, h, sub], self.scales[which][page, h, sub], c,
+                                        new[which][i:i + m, h], self.kind)
+                    self.codes[which][page, h, sub], self.scales[which][page, h, sub] = z, s
+            i += m
+
+    def row(self, table, length):
+        """Dequantised keys and values [length, h, d] of a row, float64."""
+        got = []
+        for which in range(2):
+            z = self.codes[which].astype(np.float64) * self.scales[which][..., None, None].astype(np.float64)
+            pages = [z[p].transpose(1, 2, 0, 3).reshape(PAGE, z.shape[1], -1) for p in table[:-(-length // PAGE)]]
+            got.append(torch.from_numpy(np.concatenate(pages)[:length] if pages else np.zeros((0,) + z.shape[1:2] + z.shape[-1:])))
+        return got
+
+
+class HostPages:
+    """Tables, lengths and counts as Python lists; every call returns the
+    pages it copies as (from, to)."""
+
+    def __init__(self, rows, width, pages):
+        self.width, self.tables = width, [[-1] * width for _ in range(rows)]
+        self.lens, self.refs, self.full = [0] * rows, [0] * pages, False
+
+    def _free(self):
+        return [p for p, r in enumerate(self.refs) if r == 0]
+
+    def resize(self, goals):
+        count = lambda n: -(-n // PAGE)  # noqa: E731
+        for r, goal in enumerate(goals):
+            if 0 <= goal < self.lens[r]:
+                for c in range(count(goal), count(self.lens[r])):
+                    self.refs[self.tables[r][c]] -= 1
+                    self.tables[r][c] = -1
+                self.lens[r] = goal
+        free, used, copies, refs = self._free(), 0, [], list(self.refs)
+        for r, goal in enumerate(goals):
+            if goal <= self.lens[r]:
+                continue
+            if goal > self.width * PAGE:
+                self.full = True
+                continue
+            have = count(self.lens[r])
+            part = self.lens[r] % PAGE != 0 and refs[self.tables[r][have - 1]] > 1
+            need = count(goal) - have + part
+            used += need
+            if need and used > len(free):
+                self.full = True
+                continue
+            take = free[used - need:used]
+            if part:
+                old = self.tables[r][have - 1]
+                copies.append((old, take[0]))
+                self.refs[old] -= 1
+            for j, p in enumerate(take):
+                self.tables[r][have - part + j] = p
+                self.refs[p] = 1
+            self.lens[r] = goal
+        return copies
+
+    def fork(self, src, dst):
+        old, lens, free, used, copies = [list(t) for t in self.tables], list(self.lens), self._free(), 0, []
+        for a, b in zip(src, dst):
+            if a != b:
+                for p in old[b]:
+                    if p >= 0:
+                        self.refs[p] -= 1
+        for a, b in zip(src, dst):
+            if a == b:
+                continue
+            part, whole = lens[a] % PAGE != 0, lens[a] // PAGE
+            used += part
+            if part and used > len(free):
+                self.full = True
+                self.tables[b], self.lens[b] = [-1] * self.width, 0
+                continue
+            self.tables[b] = old[a][:whole] + [-1] * (self.width - whole)
+            for p in old[a][:whole]:
+                self.refs[p] += 1
+            if part:
+                copies.append((old[a][whole], free[used - 1]))
+                self.tables[b][whole] = free[used - 1]
+                self.refs[free[used - 1]] += 1
+            self.lens[b] = lens[a]
+        return copies
+
+    def compact(self):
+        live = sum(r > 0 for r in self.refs)
+        holes = [p for p in range(live) if self.refs[p] == 0]
+        moves = [p for p in range(live, len(self.refs)) if self.refs[p] > 0]
+        to = dict(zip(moves, holes))
+        self.tables = [[to.get(p, p) for p in t] for t in self.tables]
+        for a, b in to.items():
+            self.refs[b], self.refs[a] = self.refs[a], 0
+        return live, list(to.items())

@@ -1,0 +1,300 @@
+"""The 8-bit cache: appended codes bit for bit against the definition in
+float32, attention over it against the float64 form of the stored values.
+
+Tolerance of the attention: weights in float16 (relative 2^-11), the result
+rounded once (half a unit e of its type), scores as in the prompt's tests:
+|err| <= (2^-11 + 2^-12) sum_j p_j |v_j| + e |out|."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_16973_amd as tq
+from tests.reader import HostCache, attention64, starts_of
+
+pytestmark = pytest.mark.gpu
+HALF = {torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+KINDS = ["int8", "fp8"]
+
+
+def table_of(lens, width, pages, seed):
+    r = np.random.RandomState(seed)
+    order = list(r.permutation(pages))
+    rows = [[int(order.pop()) for _ in range(-(-n // 64))] for n in lens]
+    full = [t + [-1] * (width - len(t)) for t in rows]
+    return rows, torch.tensor(full, dtype=torch.int32, device="cuda").reshape(len(lens), width)
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def new_values(counts, heads, d, dtype, seed, size=1.0, pad=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(2, sum(counts), heads * d + pad, generator=g, device="cuda") * size
+    return [t.to(dtype)[:, pad:].unflatten(1, (heads, d)) for t in x]
+
+
+def same(cache, host, layer, tables, lens):
+    """Codes and scales of every block that holds a token."""
+    now = HostCache(cache, layer)
+    for table, n in zip(tables, lens):
+        for b in range(-(-n // 16)):
+            p, sub = table[b // 4], b % 4
+            for which in range(2):
+                assert np.array_equal(now.codes[which][p, :, sub], host.codes[which][p, :, sub]), (p, sub, which)
+                assert np.array_equal(now.scales[which][p, :, sub], host.scales[which][p, :, sub]), (p, sub, which)
+
+
+def dirty(cache):
+    """Storage as it may be found: every byte pattern, NaN scales."""
+    for t in (cache.k, cache.v):
+        t.view(torch.int8).random_(-128, 128)
+    for t in (cache.k_scale, cache.v_scale):
+        t.fill_(math.nan)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("d,heads", [(64, 1), (128, 3), (256, 2)])
+@pytest.mark.parametrize("dtype,pad", [(torch.bfloat16, 0), (torch.float16, 0), (torch.float16, 3)])
+def test_append(d, heads, kind, dtype, pad):
+    cache = tq.KVCache(2, 40, heads, d, kind)
+    dirty(cache)
+    host = HostCache(cache, 1)
+    before = cache.k[0].view(torch.int8).clone()
+    width = 5
+    lens = [0] * 6
+    rows, tables = table_of([300] * 6, width, 40, 1)
+    # whole prompts, single tokens, runs that end inside blocks and pages, a growing scale, an idle row
+    for step, counts in enumerate([[1, 16, 17, 130, 64, 0], [1, 1, 1, 1, 1, 0], [15, 30, 2, 5, 64, 1], [3, 0, 47, 1, 100, 33]]):
+        new = new_values(counts, heads, d, dtype, 10 + step, 1.0 + step, pad)
+        lens = [n + c for n, c in zip(lens, counts)]
+        cache.append(1, new[0], new[1], tables, ints(lens), starts_of(counts))
+        at = 0
+        for r, c in enumerate(counts):
+            host.append([t[at:at + c].float().cpu().numpy() for t in new], rows[r], lens[r])
+            at += c
+        same(cache, host, 1, rows, lens)
+    assert torch.equal(cache.k[0].view(torch.int8), before)
+    cache.check()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_append_one_token_each_and_values_at_the_edges(kind):
+    cache = tq.KVCache(1, 8, 2, 64, kind)
+    dirty(cache)
+    host = HostCache(cache, 0)
+    rows, tables = table_of([64] * 4, 1, 8, 3)
+    vals = [0.0, 2.0 ** -120, 1e-30, 1.0, 3.0e38, -0.0, 65504.0, 2.0 ** -100]
+    lens = [0] * 4
+    for step, x in enumerate(vals):
+        new = [torch.full((4, 2, 64), x, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        new[0][:, :, ::3] *= -0.5
+        lens = [n + 1 for n in lens]
+        cache.append(0, new[0], new[1], tables, ints(lens))
+        for r in range(4):
+            host.append([t[r:r + 1].float().cpu().numpy() for t in new], rows[r], lens[r])
+        same(cache, host, 0, rows, lens)
+    cache.check()
+    for x in (math.inf, -math.inf, math.nan):
+        new = [torch.randn(4, 2, 64, device="cuda").to(torch.bfloat16) for _ in range(2)]
+        new[1][2, 1, 7] = x
+        lens = [n + 1 for n in lens]
+        cache.append(0, new[0], new[1], tables, ints(lens))
+        for r in range(4):
+            host.append([t[r:r + 1].float().cpu().numpy() for t in new], rows[r], lens[r])
+        same(cache, host, 0, rows, lens)
+        with pytest.raises(RuntimeError, match="infinite or NaN"):
+            cache.check()
+        cache.check()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_append_after_a_retreat(kind):
+    # drafted tokens are dropped and their places written again
+    cache = tq.KVCache(1, 4, 1, 128, kind)
+    dirty(cache)
+    host = HostCache(cache, 0)
+    rows, tables = table_of([128], 2, 4, 5)
+    for step, (length, n, size) in enumerate([(40, 40, 1.0), (46, 6, 1.0), (43, 2, 9.0), (45, 1, 0.1), (33, 1, 1.0)]):
+        new = new_values([n], 1, 128, torch.float16, 20 + step, size)
+        cache.append(0, new[0], new[1], tables, ints([length]), starts_of([n]))
+        host.append([t.float().cpu().numpy() for t in new], rows[0], length)
+        same(cache, host, 0, rows, [45 if step > 2 else length])
+
+
+def test_quantisation_error():
+    # half a step of the block's scale, e4m3: half a unit of 2^-3 relative
+    for kind, step in (("int8", 0.5), ("fp8", 16.0)):
+        cache = tq.KVCache(1, 4, 2, 64, kind)
+        new = new_values([200], 2, 64, torch.bfloat16, 1, 3.0)
+        rows, tables = table_of([200], 4, 4, 0)
+        cache.append(0, new[0], new[1], tables, ints([200]), starts_of([200]))
+        host = HostCache(cache, 0)
+        for got, x, s in zip(host.row(rows[0], 200), new, host.scales):
+            scale = np.concatenate([s[p].transpose(1, 0).repeat(16, 0) for p in rows[0]])[:200]
+            assert np.all(np.abs(got.numpy() - x.double().cpu().numpy()) <= step * 1.0001 * scale[..., None])
+
+
+def filled(lens, width, pages, heads, d, kind, seed=0, layers=1):
+    """A cache with random content of the rows and dirt everywhere else."""
+    cache = tq.KVCache(layers, pages, heads, d, kind)
+    dirty(cache)
+    rows, tables = table_of(lens, width, pages, seed)
+    for layer in range(layers):
+        new = new_values(lens, heads, d, torch.float16, 100 + seed + layer)
+        cache.append(layer, new[0], new[1], tables, ints(lens), starts_of(lens))
+    return cache, rows, tables
+
+
+def check_attend(cache, host, rows, lens, q, counts, out, lse, scale=None):
+    d = q.shape[2]
+    scale = 1 / math.sqrt(d) if scale is None else scale
+    e = HALF[q.dtype]
+    t = 0
+    for r, (n, c) in enumerate(zip(lens, counts)):
+        k, v = host.row(rows[r], n)
+        ref, rl, size = attention64(q[t:t + c], k, v, [n - c + i for i in range(c)], scale)
+        got, gl = out[t:t + c].double().cpu(), lse[t:t + c].double().cpu()
+        assert torch.all((got - ref).abs() <= (2.0 ** -11 + 2.0 ** -12) * size + e * ref.abs() + 2.0 ** -24), (r, n, c)
+        assert torch.equal(torch.isinf(gl), torch.isinf(rl))
+        fin = ~torch.isinf(rl)
+        assert torch.all((gl - rl)[fin].abs() <= 2.0 ** -12 + 2.0 ** -20 * rl[fin].abs())
+        t += c
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("heads,kv_heads", [(3, 3), (8, 2), (20, 1), (40, 1)])
+def test_attend_single_tokens(heads, kv_heads, d, kind):
+    lens = [1, 0, 15, 16, 17, 63, 64, 65, 300, 129, 777]
+    cache, rows, tables = filled(lens, 13, 40, kv_heads, d, kind, layers=2)
+    host = HostCache(cache, 1)
+    for dtype in (torch.float16, torch.bfloat16):
+        g = torch.Generator(device="cuda").manual_seed(5)
+        q = torch.randn(len(lens), heads, d, generator=g, device="cuda").to(dtype)
+        out, lse = cache.attend(1, q, tables, ints(lens), return_lse=True)
+        check_attend(cache, host, rows, lens, q, [1] * len(lens), out, lse)
+        again = cache.attend(1, q, tables, ints(lens), longest=777)
+        check_attend(cache, host, rows, lens, q, [1] * len(lens), again, lse)
+    cache.check()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("d,counts", [(64, [4, 1, 0, 9, 2]), (128, [4, 1, 0, 9, 2]), (256, [3, 1, 1, 2, 2]),
+                                      (64, [100, 64, 0, 33, 17]), (128, [40, 150, 1, 90, 64]), (256, [30, 64, 0, 33, 90])])
+def test_attend_several_tokens(d, counts, kind):
+    heads, kv_heads = 6, 2
+    lens = [200, 150, 0 if counts[2] == 0 else 5, 90, 64]
+    cache, rows, tables = filled(lens, 4, 20, kv_heads, d, kind)
+    counts = [min(c, n) for c, n in zip(counts, lens)]
+    host = HostCache(cache, 0)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    wide = torch.randn(sum(counts), heads * d + 5, generator=g, device="cuda").to(torch.bfloat16)
+    for q in (wide[:, 5:].unflatten(1, (heads, d)), wide[:, :heads * d].contiguous().view(-1, heads, d).half()):
+        out, lse = cache.attend(0, q, tables, ints(lens), starts_of(counts), scale=0.11, return_lse=True)
+        check_attend(cache, host, rows, lens, q, counts, out, lse, 0.11)
+
+
+def test_attend_more_queries_than_tokens():
+    # a length shorter than the row's queries: the first of them see nothing
+    cache, rows, tables = filled([3, 70], 2, 5, 1, 64, "int8")
+    q = torch.randn(8, 2, 64, device="cuda").to(torch.float16)
+    out, lse = cache.attend(0, q, tables, ints([3, 70]), starts_of([5, 3]), return_lse=True)
+    assert torch.all(out[:2] == 0) and torch.all(lse[:2] == -math.inf)
+    check_attend(cache, HostCache(cache, 0), rows, [3, 70], q, [5, 3], out, lse)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_attend_long_row(kind):
+    lens = [20011, 3, 9000]
+    cache, rows, tables = filled(lens, 313, 460, 1, 64, kind)
+    q = torch.randn(3, 4, 64, device="cuda").to(torch.float16)
+    out, lse = cache.attend(0, q, tables, ints(lens), return_lse=True)
+    check_attend(cache, HostCache(cache, 0), rows, lens, q, [1] * 3, out, lse)
+    # the same with a few queries, and cut at `longest`
+    q = torch.randn(9, 4, 64, device="cuda").to(torch.bfloat16)
+    out, lse = cache.attend(0, q, tables, ints(lens), starts_of([4, 1, 4]), return_lse=True)
+    check_attend(cache, HostCache(cache, 0), rows, lens, q, [4, 1, 4], out, lse)
+    out = cache.attend(0, q[:3], tables, ints(lens), longest=5000)
+    cut = cache.attend(0, q[:3], tables, ints([5000, 3, 5000]), longest=5000)
+    assert torch.equal(out, cut)
+
+
+def test_attend_queries_of_any_size():
+    # float16 with one power of two per row: tiny, huge and mixed queries
+    cache, rows, tables = filled([100] * 5, 2, 12, 1, 64, "int8")
+    host = HostCache(cache, 0)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    q = torch.randn(5, 2, 64, generator=g, device="cuda")
+    q[1] *= 1e-20
+    q[2] *= 1e-36
+    q[3] *= 1e18
+    q[4, :, ::2] *= 1e-6
+    q = q.to(torch.bfloat16)
+    out, lse = cache.attend(0, q, tables, ints([100] * 5), return_lse=True)
+    for r in (0, 1, 2, 4):
+        check_attend(cache, host, [rows[r]], [100], q[r:r + 1], [1], out[r:r + 1], lse[r:r + 1])
+    assert torch.isfinite(out[3]).all()    # one key takes all
+    q[0, 0, 3] = math.nan
+    q[4, 1, 3] = math.inf
+    bad = cache.attend(0, q, tables, ints([100] * 5))
+    assert torch.isnan(bad[0, 0]).all() and torch.isnan(bad[4, 1]).all()
+    assert torch.equal(bad[1:4], out[1:4]) and torch.equal(bad[0, 1], out[0, 1]) and torch.equal(bad[4, 0], out[4, 0])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_scales_of_very_different_size(kind):
+    # values of one block 1e6 times those of another: each block has its own scale
+    cache = tq.KVCache(1, 6, 1, 64, kind)
+    dirty(cache)
+    rows, tables = table_of([200], 4, 6, 2)
+    new = new_values([200], 1, 64, torch.float16, 3)
+    size = torch.tensor([1.0, 1e-4, 100.0, 1e-2] * 4, device="cuda").repeat_interleave(16)[:200, None, None]
+    v = (new[1].float() * size).to(torch.float16)
+    cache.append(0, new[0], v, tables, ints([200]), starts_of([200]))
+    q = torch.randn(1, 3, 64, device="cuda").to(torch.float16)
+    out, lse = cache.attend(0, q, tables, ints([200]), return_lse=True)
+    check_attend(cache, HostCache(cache, 0), rows, [200], q, [1], out, lse)
+
+
+def test_bad_page_ids_are_left_out():
+    cache, rows, tables = filled([200], 4, 6, 1, 64, "int8")
+    q = torch.randn(1, 2, 64, device="cuda").to(torch.float16)
+    broken = tables.clone()
+    broken[0, 1] = 6
+    broken[0, 2] = -1
+    out, lse = cache.attend(0, q, broken, ints([200]), return_lse=True)
+    k, v = HostCache(cache, 0).row(rows[0], 200)
+    keep = [i for i in range(200) if i // 64 in (0, 3)]
+    ref, rl, size = attention64(q, k[keep], v[keep], [len(keep)], 1 / 8)
+    assert torch.all((out.double().cpu() - ref).abs() <= 2.0 ** -10 * size + 2.0 ** -11 * ref.abs())
+    with pytest.raises(RuntimeError, match="outside the pool"):
+        cache.check()
+    new = new_values([1], 1, 64, torch.float16, 9)
+    before = cache.k.view(torch.int8).clone()
+    cache.append(0, new[0], new[1], broken, ints([100]))
+    assert torch.equal(cache.k.view(torch.int8), before)
+    with pytest.raises(RuntimeError, match="outside the pool"):
+        cache.check()
+
+
+def test_graph_of_a_step():
+    cache, rows, tables = filled([100, 40], 3, 8, 2, 64, "int8")
+    lens = ints([101, 41])
+    new = new_values([1, 1], 2, 64, torch.bfloat16, 12)
+    q = torch.randn(2, 4, 64, device="cuda").to(torch.bfloat16)
+    cache.append(0, new[0], new[1], tables, lens)
+    eager = cache.attend(0, q, tables, lens)
+    out = torch.empty_like(eager)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.append(0, new[0], new[1], tables, lens)
+        cache.attend(0, q, tables, lens, out=out)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)
+        cache.attend(0, q, tables, lens)
