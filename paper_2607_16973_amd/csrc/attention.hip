@@ -8,27 +8,40 @@
 // correction are lane values, and the weights a lane computes are the operand
 // the second product wants from it when its keys are taken in the order
 // S^T hands them out: 8 j + 4 (lane / 32) + i, so P never leaves the registers.
-// Bound by the matrix cores and the exponentials.
+// V^T comes out of LDS through transposing reads (4 keys of a coordinate per
+// lane).  Keys and values of the next step are loaded straight into the other
+// half of LDS while this one is used; one barrier per step.  16-byte pieces
+// of a row are exchanged by the row's low bits so that neither read meets
+// bank conflicts.
+// The running maximum follows only when a score passes it by 2^kLag: until
+// then weights grow up to 2^kLag instead of the accumulators being rescaled.
 #include <hip/hip_runtime.h>
 
 #include "kv.h"
+#include "lds_dma.h"
 
 namespace tq {
 namespace {
 
 constexpr int kKeys = 64;     // keys of a step
 constexpr int kRows = 128;    // query rows of a workgroup
+constexpr float kLag = 8.f;   // log2 of the weight at which the maximum must follow
 
 template <bool BF16>
 struct Half;
 template <>
 struct Half<true> {
     typedef bf16x8 x8;
+    typedef __bf16 x1;
+    static constexpr float kBias = 0.f;
     static __device__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 template <>
 struct Half<false> {
     typedef f16x8 x8;
+    typedef _Float16 x1;
+    // weights are held in units of 2^-6: float16 keeps 11 bits of them down to 2^-20
+    static constexpr float kBias = 6.f;
     static __device__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 
@@ -38,13 +51,38 @@ __device__ inline bool finite16(unsigned short u) {
     return (u & e) != e;
 }
 
-template <int D, bool BF16>
-__global__ __launch_bounds__(256) void prompt_kernel(PromptArgs a) {
+__device__ inline float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+// Piece of a row at which piece c of key row kr lies.
+template <int CH>
+__device__ inline int k_piece(int kr, int c) { return c ^ (kr & (CH - 1) & 15); }
+template <int CH>
+__device__ inline int v_piece(int kr, int c) { return c ^ ((kr & (CH / 2 - 1) & 7) << 1); }
+
+// Transposing LDS read: of 16 lanes, lane 4 j + c names 4 coordinates (8 bytes) of
+// key j; lane i receives coordinate i of the four keys.
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+__device__ inline u32x2 read_transposed(uint32_t at) {
+    const s16x4 r = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) s16x4 *)(uintptr_t)at);
+    return __builtin_bit_cast(u32x2, r);
+}
+
+// WIDE: 16-byte loads are aligned, so that rows can go straight into LDS.
+template <int D, bool BF16, bool WIDE>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void prompt_kernel(PromptArgs a) {
     typedef typename Half<BF16>::x8 x8;
     constexpr int KS = D / 16, DT = D / 32, CH = D / 8;   // CH: 16-byte pieces of a row
-    __shared__ __align__(16) unsigned short kl[kKeys * D], vl[kKeys * D];
+    constexpr int TILE = kKeys * D * 2;                   // bytes of a step's keys
+    extern __shared__ __align__(16) char lds[];           // [2][keys, values]
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int n = lane & 31, h = lane >> 5;
+
     // key heads next to each other: workgroups go round the XCDs, so one
     // XCD's L2 sees few of the heads' keys.  A row's long tiles come first.
     const int kvh = blockIdx.x % a.kv_heads;
@@ -60,108 +98,168 @@ __global__ __launch_bounds__(256) void prompt_kernel(PromptArgs a) {
     const int64_t r = slot * kRows + wave * 32 + n;
     const bool in = r < rows;
     const int token = in ? (int)(r / a.group) : 0, head = kvh * a.group + (in ? (int)(r % a.group) : 0);
-    // last key the query sees, and the last one any row of the workgroup sees
+    // last key the query sees, the last one any row of the workgroup sees, and
+    // the last one that all of them see
     const int pos = !in ? -1 : a.causal ? token + keys - count : keys - 1;
     const int64_t last_row = min(rows, (slot + 1) * kRows) - 1;
     const int top = a.causal ? (int)(last_row / a.group) + keys - count : keys - 1;
+    const int full = a.causal ? (int)(slot * kRows / a.group) + keys - count : keys - 1;
+    const int steps = top < 0 ? 0 : top / kKeys + 1;
 
+    // a negative scale is one of the negated queries: the largest product has the largest score
+    const float c2 = fabsf(a.scale2);
+    const unsigned flip = a.scale2 < 0.f ? 0x80008000u : 0u;
     x8 q[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-        unsigned short u[8];
         const unsigned short *p = static_cast<const unsigned short *>(a.q) + (int64_t)(first + token) * a.qt + head * a.qh + s * 16 + h * 8;
-        for (int j = 0; j < 8; ++j) u[j] = in ? p[j] : 0;
-        __builtin_memcpy(&q[s], u, 16);
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (in) {
+            if constexpr (WIDE) u = *reinterpret_cast<const uint4 *>(p);
+            else __builtin_memcpy(&u, p, 16);
+        }
+        u.x ^= flip, u.y ^= flip, u.z ^= flip, u.w ^= flip;
+        q[s] = __builtin_bit_cast(x8, u);
     }
+
+    // The rows of a step into half `to` of LDS; past the last key its row
+    // again (its scores are masked).
+    const unsigned short *kbase = static_cast<const unsigned short *>(a.k) + (int64_t)kfirst * a.kt + (int64_t)kvh * a.kh;
+    const unsigned short *vbase = static_cast<const unsigned short *>(a.v) + (int64_t)kfirst * a.vt + (int64_t)kvh * a.vh;
+    auto stage = [&](int k0, int to) {
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int i = 0; i < CH / 4; ++i) {            // 64 pieces each: kKeys * CH / 256 of a wave
+                const int first_piece = (i * 4 + wave) * 64, at = first_piece + lane;
+                const int kr = at / CH, p = at % CH, key = min(k0 + kr, keys - 1);
+                const unsigned short *ks = kbase + key * a.kt + k_piece<CH>(kr, p) * 8;
+                const unsigned short *vs = vbase + key * a.vt + v_piece<CH>(kr, p) * 8;
+                lds_dma16(ks, lds0 + to * 2 * TILE + first_piece * 16);
+                lds_dma16(vs, lds0 + to * 2 * TILE + TILE + first_piece * 16);
+            }
+        } else {
+            for (int at = threadIdx.x; at < kKeys * CH; at += 256) {
+                const int kr = at / CH, p = at % CH, key = min(k0 + kr, keys - 1);
+                uint4 ku, vu;
+                __builtin_memcpy(&ku, __builtin_assume_aligned(kbase + key * a.kt + p * 8, 2), 16);
+                __builtin_memcpy(&vu, __builtin_assume_aligned(vbase + key * a.vt + p * 8, 2), 16);
+                char *base = lds + to * 2 * TILE;
+                *reinterpret_cast<uint4 *>(base + (kr * CH + k_piece<CH>(kr, p)) * 16) = ku;
+                *reinterpret_cast<uint4 *>(base + TILE + (kr * CH + v_piece<CH>(kr, p)) * 16) = vu;
+            }
+        }
+    };
+
     f32x16 o[DT];
+#pragma unroll
     for (int d = 0; d < DT; ++d)
         for (int j = 0; j < 16; ++j) o[d][j] = 0.f;
     float m = -__builtin_inff(), l = 0.f;
+    float shift = 0.f;                                    // bias - m c2
 
-    const int full = a.causal ? (int)(slot * kRows / a.group) + keys - count : keys - 1;   // keys that all rows see
-    for (int k0 = 0; k0 <= top; k0 += kKeys) {
-        const bool masked = k0 + kKeys - 1 > full;
-        bool odd = false;
+    // LDS addresses within a half: key rows n (+ 32 t), value rows 4 h + s / 4 (+ 8)
+    uint32_t kat[KS], vat[DT];
+#pragma unroll
+    for (int c = 0; c < KS; ++c) kat[c] = lds0 + (n * CH + k_piece<CH>(n, 2 * c + h)) * 16;
+    {
+        const int s = lane & 15, kr = 4 * h + (s >> 2);
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+            vat[d] = lds0 + TILE + (kr * CH + v_piece<CH>(kr, d * 4 + ((lane >> 4) & 1) * 2 + ((s & 3) >> 1))) * 16 + (s & 1) * 8;
+    }
+
+    if (steps) stage(0, 0);
+    for (int step = 0; step < steps; ++step) {
+        const int k0 = step * kKeys;
+        const uint32_t half = (step & 1) * 2 * TILE;
+        wait_vmem<0>();
         __syncthreads();
-        for (int c = threadIdx.x; c < kKeys * CH; c += 256) {
-            const int kr = c / CH, piece = c % CH, key = k0 + kr;
-            unsigned short uk[8], uv[8];
-            for (int j = 0; j < 8; ++j) uk[j] = uv[j] = 0;
-            if (key < keys) {
-                const unsigned short *pk = static_cast<const unsigned short *>(a.k) + (int64_t)(kfirst + key) * a.kt + kvh * a.kh + piece * 8;
-                const unsigned short *pv = static_cast<const unsigned short *>(a.v) + (int64_t)(kfirst + key) * a.vt + kvh * a.vh + piece * 8;
-                for (int j = 0; j < 8; ++j) uk[j] = pk[j], uv[j] = pv[j];
-            }
-            __builtin_memcpy(&kl[kr * D + (piece ^ (kr % CH)) * 8], uk, 16);
-            __builtin_memcpy(&vl[kr * D + piece * 8], uv, 16);
-            for (int j = 0; j < 8; ++j) odd |= !finite16<BF16>(uv[j]);
-        }
+        if (step + 1 < steps) stage(k0 + kKeys, (step + 1) & 1);
+
         // Values that are not finite must not meet the zero weights of the
         // rows that do not see them: where a step has both, they are taken
         // out of the product and added to the rows that do see them.
-        odd = __syncthreads_or(odd && masked);
+        const bool masked = k0 + kKeys - 1 > full;
+        bool odd = false;
+        if (masked) {
+            for (int i = threadIdx.x; i < kKeys * CH; i += 256) {
+                const uint4 u = *reinterpret_cast<const uint4 *>(lds + half + TILE + i * 16);
+                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+                for (int j = 0; j < 4; ++j) odd |= !finite16<BF16>(w[j] & 0xffff) || !finite16<BF16>(w[j] >> 16);
+            }
+            odd = __syncthreads_or(odd);
+        }
+
         f32x16 s[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < 2; ++t)
             for (int j = 0; j < 16; ++j) s[t][j] = 0.f;
 #pragma unroll
-            for (int c = 0; c < KS; ++c) {
-                x8 k;
-                const int kr = t * 32 + n, piece = 2 * c + h;
-                __builtin_memcpy(&k, &kl[kr * D + (piece ^ (kr % CH)) * 8], 16);
+        for (int c = 0; c < KS; ++c)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const x8 k = *(__attribute__((address_space(3))) const x8 *)(uintptr_t)(kat[c] + half + t * 32 * CH * 16);
                 s[t] = Half<BF16>::mfma(k, q[c], s[t]);
             }
-        }
-        float big = -__builtin_inff();
-        float y[32];
+        if (masked) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const int key = k0 + (j >> 4) * 32 + ((j & 15) >> 2) * 8 + 4 * h + (j & 3);
-            float z = s[j >> 4][j & 15] * a.scale2;
-            if (key > pos) z = -__builtin_inff();
-            y[j] = z;
-            big = fmaxf(big, z);
-        }
-        const float mn = fmaxf(m, max_of_halves(big)), mm = mn == -__builtin_inff() ? 0.f : mn;
-        const float alpha = __builtin_amdgcn_exp2f(m - mm);
-        float sum = 0.f;
-        unsigned short pw[32];
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const float e = __builtin_amdgcn_exp2f(y[j] - mm);
-            sum += e;
-            pw[j] = float_bits16(e, BF16);
-        }
-        l = l * alpha + sum;
-        m = mn;
-        for (int d = 0; d < DT; ++d) o[d] *= alpha;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {   // 16 keys: lane half h has 4h + i and 8 + 4h + i of them
-            x8 p;
-            __builtin_memcpy(&p, &pw[8 * c], 16);
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                unsigned short u[8];
-                for (int i = 0; i < 4; ++i) {
-                    u[i] = vl[(16 * c + 4 * h + i) * D + d * 32 + n];
-                    u[4 + i] = vl[(16 * c + 8 + 4 * h + i) * D + d * 32 + n];
-                }
-                if (odd)
-                    for (int i = 0; i < 8; ++i) u[i] = finite16<BF16>(u[i]) ? u[i] : 0;
-                x8 v;
-                __builtin_memcpy(&v, u, 16);
-                o[d] = Half<BF16>::mfma(v, p, o[d]);
+            for (int j = 0; j < 32; ++j) {
+                const int key = k0 + (j >> 4) * 32 + ((j & 15) >> 2) * 8 + 4 * h + (j & 3);
+                if (key > pos) s[j >> 4][j & 15] = -__builtin_inff();
             }
         }
+        float big = max3(s[0][0], s[0][1], s[0][2]);
+#pragma unroll
+        for (int j = 3; j < 31; j += 2) big = max3(big, s[j >> 4][j & 15], s[(j + 1) >> 4][(j + 1) & 15]);
+        big = max_of_halves(fmaxf(big, s[1][15]));
+        if (__any((big - m) * c2 > kLag || (m == -__builtin_inff() && big > m))) {
+            const float mn = fmaxf(m, big), mm = mn == -__builtin_inff() ? 0.f : mn;
+            const float alpha = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m - mm) * c2);
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] *= alpha;
+            m = mn;
+            shift = Half<BF16>::kBias - mm * c2;
+        }
+        typename Half<BF16>::x1 pw[32];
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j >> 4][j & 15], c2, shift));
+            sum[j & 1] += e;
+            pw[j] = (typename Half<BF16>::x1)e;
+        }
+        l += sum[0] + sum[1];
         if (odd) {
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
                     for (int kr = 0; kr < kKeys && k0 + kr <= pos; ++kr) {
-                        const unsigned short u = vl[kr * D + d * 32 + (j >> 2) * 8 + 4 * h + (j & 3)];
+                        const int e = d * 32 + (j >> 2) * 8 + 4 * h + (j & 3);
+                        const unsigned short u = *reinterpret_cast<const unsigned short *>(
+                            lds + half + TILE + (kr * CH + v_piece<CH>(kr, e >> 3)) * 16 + (e & 7) * 2);
                         if (!finite16<BF16>(u)) o[d][j] += BF16 ? bf16_float(u) : f16_float(u);
                     }
+            __syncthreads();
+            for (int i = threadIdx.x; i < kKeys * D; i += 256) {
+                unsigned short *u = reinterpret_cast<unsigned short *>(lds + half + TILE) + i;
+                if (!finite16<BF16>(*u)) *u = 0;
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {   // 16 keys: lane half h has 4h + i and 8 + 4h + i of them
+            x8 p;
+            for (int i = 0; i < 8; ++i) p[i] = pw[8 * c + i];
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                const u32x2 lo = read_transposed(vat[d] + half + (16 * c) * CH * 16);
+                const u32x2 hi = read_transposed(vat[d] + half + (16 * c + 8) * CH * 16);
+                uint32_t w[4] = {lo.x, lo.y, hi.x, hi.y};
+                x8 v;
+                __builtin_memcpy(&v, w, 16);
+                o[d] = Half<BF16>::mfma(v, p, o[d]);
+            }
         }
     }
     if (!in) return;
@@ -177,22 +275,33 @@ __global__ __launch_bounds__(256) void prompt_kernel(PromptArgs a) {
             for (int i = 0; i < 4; ++i) u[i] = float_bits16(o[d][4 * j + i] * inv, BF16);
             __builtin_memcpy(static_cast<unsigned short *>(a.out) + at * D + d * 32 + 8 * j + 4 * h, u, 8);
         }
-    if (a.lse && h == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * 0.69314718056f;
+    if (a.lse && h == 0)
+        a.lse[at] = l == 0.f ? -__builtin_inff() : (m * c2 + (__log2f(l) - Half<BF16>::kBias)) * 0.69314718056f;
 }
 
-template <int D>
-hipError_t launch(const PromptArgs &a, int bf16, hipStream_t stream) {
+template <int D, bool BF16, bool WIDE>
+hipError_t launch(const PromptArgs &a, hipStream_t stream) {
     const int64_t slots = (int64_t)a.total * a.group / kRows + a.rows;
     const unsigned grid = (unsigned)(slots * a.kv_heads);
-    if (bf16) prompt_kernel<D, true><<<grid, 256, 0, stream>>>(a);
-    else prompt_kernel<D, false><<<grid, 256, 0, stream>>>(a);
+    constexpr int lds = 4 * kKeys * D * 2;
+    if (lds > 65536) {
+        static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(prompt_kernel<D, BF16, WIDE>),
+                                                           hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (once != hipSuccess) return once;
+    }
+    prompt_kernel<D, BF16, WIDE><<<grid, 256, lds, stream>>>(a);
     return hipGetLastError();
+}
+template <int D>
+hipError_t pick(const PromptArgs &a, int bf16, hipStream_t stream) {
+    if (bf16) return a.wide ? launch<D, true, true>(a, stream) : launch<D, true, false>(a, stream);
+    return a.wide ? launch<D, false, true>(a, stream) : launch<D, false, false>(a, stream);
 }
 
 }  // namespace
 
 hipError_t prompt_attention(const PromptArgs &a, int D, int bf16, hipStream_t stream) {
-    return D == 64 ? launch<64>(a, bf16, stream) : D == 128 ? launch<128>(a, bf16, stream) : launch<256>(a, bf16, stream);
+    return D == 64 ? pick<64>(a, bf16, stream) : D == 128 ? pick<128>(a, bf16, stream) : pick<256>(a, bf16, stream);
 }
 
 }  // namespace tq

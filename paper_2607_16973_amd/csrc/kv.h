@@ -62,7 +62,7 @@ struct PromptArgs {
     const void *q, *k, *v;
     int64_t qt, qh, kt, kh, vt, vh;
     const int *starts, *key_starts;
-    int rows, total, keys, heads, group, kv_heads, causal;
+    int rows, total, keys, heads, group, kv_heads, causal, wide;
     float scale2;
     void *out;
     float *lse;

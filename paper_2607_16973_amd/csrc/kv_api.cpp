@@ -303,6 +303,7 @@ tq_status tq_attention(const tq_rows *q, const tq_rows *k, const tq_rows *v, int
         a.group = group;
         a.kv_heads = kv_heads;
         a.causal = causal;
+        a.wide = wide_rows(q) && wide_rows(k) && wide_rows(v);
         a.scale2 = scale * 1.44269504089f;
         a.out = out;
         a.lse = lse;
