@@ -33,6 +33,7 @@ HIP_SOURCES = ["encode.hip", "scan.hip", "batch.hip", "layout.hip", "calib.hip",
 EXTRA_FLAGS = {"encode.hip": ["-mllvm", "-disable-machine-sink"],
                "scan.hip": ["-mllvm", "-disable-machine-sink",
                             "-mllvm", "-amdgpu-atomic-optimizer-strategy=None"],
+               "kv_attend.hip": ["-mllvm", "-disable-machine-sink"],
                "batch.hip": ["-mllvm", "-disable-machine-sink",
                              "-mllvm", "-amdgpu-atomic-optimizer-strategy=None"]}
 HOST_SOURCES = ["codebook.cpp", "rotation.cpp"]

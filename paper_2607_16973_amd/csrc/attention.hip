@@ -156,6 +156,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void prompt_kernel(PromptArg
         for (int j = 0; j < 16; ++j) o[d][j] = 0.f;
     float m = -__builtin_inff(), l = 0.f;
     float shift = 0.f;                                    // bias - m c2
+    bool wild = false;                                    // m c2 so large that its rounding shows
 
     // LDS addresses within a half: key rows n (+ 32 t), value rows 4 h + s / 4 (+ 8)
     uint32_t kat[KS], vat[DT];
@@ -219,12 +220,21 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void prompt_kernel(PromptArg
             for (int d = 0; d < DT; ++d) o[d] *= alpha;
             m = mn;
             shift = Half<BF16>::kBias - mm * c2;
+            wild = __any(fabsf(mm * c2) > 0x1p20f);
+        }
+        float c1 = c2, s1 = shift;
+        if (wild) {   // both products rounded alike: the largest score gives 0
+            const float mm = m == -__builtin_inff() ? 0.f : m * c2;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) s[j >> 4][j & 15] = scaled_less(s[j >> 4][j & 15], c2, mm);
+            c1 = 1.f;
+            s1 = Half<BF16>::kBias;
         }
         typename Half<BF16>::x1 pw[32];
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
-            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j >> 4][j & 15], c2, shift));
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j >> 4][j & 15], c1, s1));
             sum[j & 1] += e;
             pw[j] = (typename Half<BF16>::x1)e;
         }

@@ -50,9 +50,9 @@ struct AttendArgs {
     int chunks, chunk_pages;      // the pages of a row in so many parts
     int limit;                    // tokens of a row that are looked at
 };
-// How a call is split: query rows per workgroup, pages per part.
+// How a call is split: query rows and waves per workgroup, pages per part.
 struct AttendPlan {
-    int tile, rows_apart, chunks, chunk_pages;
+    int tile, waves, chunks, chunk_pages;
 };
 AttendPlan attend_plan(int64_t n, int rows, int group, int kv_heads, int width, int longest, int D);
 size_t attend_part_bytes(const AttendPlan &p, int64_t n, int heads, int D);
@@ -111,14 +111,20 @@ __device__ inline void row_tokens(const int *starts, int i, int total, int *firs
 __device__ inline int64_t slot_begin(const int *starts, int i, int num, int den, int extra) {
     return (int64_t)starts[i] * num / den + (int64_t)i * extra;
 }
+// Called by whole waves: the 64 lanes look at 64 places at once, so up to 64
+// rows take one round of loads, up to 4,096 two.
 __device__ inline int slot_row(const int *starts, int rows, int64_t s, int num, int den, int extra) {
-    int lo = 0, hi = rows - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (slot_begin(starts, mid, num, den, extra) <= s) lo = mid;
-        else hi = mid - 1;
+    const int lane = __lane_id();
+    int lo = 0, n = rows;
+    while (n > 1) {
+        const int step = (n + 63) >> 6, i = lane * step;
+        const bool le = i < n && slot_begin(starts, lo + i, num, den, extra) <= s;
+        const int past = __popcll(__ballot(le));
+        if (past == 0) break;
+        lo += (past - 1) * step;
+        n = min(step, n - (past - 1) * step);
     }
-    return lo;
+    return __builtin_amdgcn_readfirstlane(lo);
 }
 
 // Largest / sum over the lanes l, l ^ 16, l ^ 32, l ^ 48.
@@ -142,6 +148,14 @@ __device__ inline float max_of_halves(float x) {
 __device__ inline float sum_of_halves(float x) {
     auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+// x * f - m with both steps rounded: never fused, so that a value gives
+// exactly 0 against its own rounded product.
+__device__ inline float scaled_less(float x, float f, float m) {
+#pragma clang fp contract(off)
+    const float y = x * f;
+    return y - m;
 }
 
 __device__ inline float bf16_float(unsigned short h) { return __uint_as_float((unsigned)h << 16); }

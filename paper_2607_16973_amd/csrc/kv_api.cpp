@@ -105,6 +105,9 @@ tq_status pool_args(const tq_kv_rows *r, const tq_kv_cache *c, int64_t n, void *
     if (!r->refs_dev || (r->rows > 0 && (!r->lens_dev || (r->width > 0 && !r->tables_dev))))
         return fail(TQ_EINVAL, "rows: NULL device pointer");
     if (n < 0 || n > kMost || (n > 0 && n * r->width > kMost)) return fail(TQ_EINVAL, "n out of range");
+    // the copies' grid: pieces of 16 KiB of two stores along y
+    if (2 * (int64_t)c->layers * (((int64_t)c->kv_heads * kPage * c->head_dim + 16383) / 16384) > 65535)
+        return fail(TQ_EUNSUPPORTED, "a page of all layers is over 512 MiB");
     if (!ws || bytes < kv_rows_bytes(r->pages, r->rows, r->width, n)) return fail(TQ_EINVAL, "workspace too small");
     if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(TQ_EINVAL, "workspace not aligned");
     a->tables = r->tables_dev;
@@ -190,7 +193,7 @@ tq_status tq_kv_attend(const tq_kv_cache *cache, int32_t layer, const tq_rows *q
         const size_t need = attend_part_bytes(p, n, heads, cache->head_dim);
         if (need && (!ws || ws_bytes < need || !aligned16(ws))) return fail(TQ_EINVAL, "workspace too small or not aligned");
         if ((n * group / p.tile + (int64_t)rows * ((group + p.tile - 1) / p.tile)) * p.chunks >= kMostGroups ||
-            n * heads >= 4 * kMostGroups || n * group > kMost)
+            n * heads >= kMostGroups || n * group > kMost)
             return fail(TQ_EUNSUPPORTED, "too many queries for one call");
         if ((st = device_ready()) != TQ_OK) return st;
         AttendArgs a;

@@ -16,9 +16,11 @@
 //
 // Codes become float16 exactly (|z| <= 448).  Queries are brought to float16
 // with one power of two per row that puts the largest at 2^14: what float16
-// rounds away is 2^-39 of it.  Weights are rounded to float16 in units of
-// 2^-kUnit and of a power of two no smaller than the value scales seen so far, which
-// keeps 11 bits down to 2^-20 of the largest weight.
+// rounds away is 2^-39 of it.  The numerator has a running maximum of its own, over score +
+// log2(value scale), so that weights times value scales stay in float16's
+// range whatever the scales are; they are taken to the product in two
+// float16 parts (22 bits: the product is far from its limit here, and the rounding of the weights
+// would otherwise be as large as that of a float16 result).
 #include <hip/hip_runtime.h>
 
 #include "kv.h"
@@ -26,8 +28,19 @@
 namespace tq {
 namespace {
 
-constexpr int kUnit = 6;          // weights are at most 2^kUnit in float16
-constexpr int kNoScale = -4096;   // exponent of "no value scale yet"
+#ifndef WANT
+#define WANT 4096
+#define WHOLE 32
+#endif
+
+constexpr float kUnit = 6.f;      // weights are held in units of 2^-kUnit ...
+constexpr float kLag = 8.f;       // ... and may pass the running maximum by 2^kLag before it follows
+
+__device__ inline float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
 
 // 16 codes -> 2 x 8 float16.
 template <bool FP8>
@@ -71,122 +84,130 @@ __device__ inline uint4 keep_tokens(uint4 c, int n) {
     return c;
 }
 
-// What a wave has of a tile of 16 query rows after some pages.
+// Queries of 16 rows as operands, 8 coordinates (s/2) 64 + g 16 + (s%2) 8 of
+// each step, in float16 with the power of two that is returned.
 template <int D>
-struct Part {
-    float m, l;                 // running maximum (log2 units) and the lane's share of the sum
-    f32x4 o[D / 16];            // in units of 2^-kUnit 2^k of the wave
-};
+__device__ inline int load_queries(const AttendArgs &a, bool in, int64_t at, int g, f16x8 *q) {
+    constexpr int KS = D / 32;
+    float x[KS][8];
+    float big = 0.f;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+        if (in) load8(a.q, at + (s >> 1) * 64 + g * 16 + (s & 1) * 8, a.bf16, a.wide, x[s]);
+        else for (int j = 0; j < 8; ++j) x[s][j] = 0.f;
+        for (int j = 0; j < 8; ++j) {
+            const float y = fabsf(x[s][j]);
+            big = fmaxf(big, y < __builtin_inff() ? y : 0.f);
+        }
+    }
+    big = max_of_groups(big);
+    int e;
+    frexpf(big, &e);
+    e = big > 0.f ? 15 - e : 0;
+    const float sign = a.scale2 < 0.f ? -1.f : 1.f;
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+        for (int j = 0; j < 8; ++j) q[s][j] = (_Float16)(sign * ldexpf(x[s][j], e));
+    return e;
+}
 
-// The query rows of a tile and their position limits.
-struct Tile {
-    int row, kvh;               // row of the table, key head
-    int first, count;           // its new tokens in the packed tensor
-    int len;
-    int r0;                     // first (token, head) row of the tile within the row's
-};
-
-// NT tiles of 16 query rows per wave.  APART: every wave has rows of its own
-// and walks all pages of the part; else the four waves share the rows, take
-// every fourth page, and are joined through LDS.
-template <int D, bool FP8, int NT, bool APART>
-__global__ __launch_bounds__(256) void attend_kernel(AttendArgs a) {
+// Rows of few queries (decoding, drafted tokens): NT tiles of 16 query rows that
+// the W waves of the workgroup share.  Each wave takes every W-th page and
+// has the next one's codes on the way while it works; the waves are joined
+// through LDS.  Bound by the memory system: 16 pages of 64 D bytes in
+// flight per compute unit.
+template <int D, bool FP8, int NT, int W>
+__global__ __launch_bounds__(64 * W) void attend_kernel(AttendArgs a) {
     constexpr int KS = D / 32;                       // 32-wide steps of the first product
     constexpr int DT = D / 16;
-    constexpr int RW = 16 * NT;                      // rows of a wave
-    constexpr int RT = APART ? 4 * RW : RW;          // rows of the workgroup
+    constexpr int RT = 16 * NT;                      // rows of the workgroup
     extern __shared__ __align__(16) float lds[];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int n = lane & 15, g = lane >> 4;
 
-    Tile t;
     int64_t slot = blockIdx.x / a.chunks;
-    const int chunk = blockIdx.x % a.chunks;
-    t.kvh = blockIdx.y;
+    const int chunk = blockIdx.x % a.chunks, kvh = blockIdx.y;
+    int row, first, count;
     if (a.set.starts) {
-        t.row = slot_row(a.set.starts, a.set.rows, slot, a.group, RT, 1);
-        slot -= slot_begin(a.set.starts, t.row, a.group, RT, 1);
+        row = slot_row(a.set.starts, a.set.rows, slot, a.group, RT, 1);
+        slot -= slot_begin(a.set.starts, row, a.group, RT, 1);
     } else {   // one token per row: its group in ceil(group / RT) tiles
         const int per = (a.group + RT - 1) / RT;
-        t.row = (int)(slot / per);
+        row = (int)(slot / per);
         slot %= per;
     }
-    row_tokens(a.set.starts, t.row, a.set.total, &t.first, &t.count);
-    const int rows = t.count * a.group;
+    row_tokens(a.set.starts, row, a.set.total, &first, &count);
+    const int rows = count * a.group;
     if (slot < 0 || slot * RT >= rows) return;       // the whole workgroup
-    t.r0 = (int)slot * RT + (APART ? wave * RW : 0);
-    const int true_len = a.set.lens[t.row];
-    t.len = min(true_len, a.limit);
+    const int r0 = (int)slot * RT;
+    const int true_len = a.set.lens[row];
+    const int len = min(true_len, a.limit);
 
-    // queries: rows r0 + 16 i + n, 8 coordinates (ks/2) 64 + g 16 + (ks%2) 8 of each step
-    f16x8 q[NT][KS];
-    float factor[NT];
-    int pos[NT];
-    int top = -1;                                    // last position any row of the wave sees
+    // positions: the last key that each row, any row and every row sees
+    int pos[NT], token[NT];
+    const int last = min(rows - 1, r0 + RT - 1);
+    const int top = min(true_len - count + last / a.group, len - 1);
+    const int low = min(true_len - count + r0 / a.group, len - 1);
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-        const int r = t.r0 + 16 * i + n;
-        const bool in = r < rows;
-        const int token = in ? r / a.group : 0, head = t.kvh * a.group + (in ? r % a.group : 0);
-        pos[i] = in ? min(true_len - t.count + token, t.len - 1) : -1;
-        float x[KS][8];
-        float big = 0.f;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            if (in) load8(a.q, (t.first + token) * a.qt + head * a.qh + (s >> 1) * 64 + g * 16 + (s & 1) * 8, a.bf16, a.wide, x[s]);
-            else for (int j = 0; j < 8; ++j) x[s][j] = 0.f;
-            for (int j = 0; j < 8; ++j) {
-                const float y = fabsf(x[s][j]);
-                big = fmaxf(big, y < __builtin_inff() ? y : 0.f);
-            }
-        }
-        big = max_of_groups(big);
-        int e;
-        frexpf(big, &e);
-        e = big > 0.f ? 15 - e : 0;
-#pragma unroll
-        for (int s = 0; s < KS; ++s)
-            for (int j = 0; j < 8; ++j) q[i][s][j] = (_Float16)ldexpf(x[s][j], e);
-        factor[i] = ldexpf(a.scale2, -e);
-        top = max(top, pos[i]);
+        token[i] = min(r0 + 16 * i + n, last) / a.group;
+        pos[i] = min(true_len - count + token[i], len - 1);
     }
-    for (int m = 1; m < 16; m <<= 1) top = max(top, __shfl_xor(top, m));
-    top = __builtin_amdgcn_readfirstlane(top);
+    const int begin = chunk * a.chunk_pages + wave;
+    const int end = top < 0 ? 0 : min(top / kPage + 1, (chunk + 1) * a.chunk_pages);
 
-    Part<D> part[NT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        part[i].m = -__builtin_inff();
-        part[i].l = 0.f;
-        for (int d = 0; d < DT; ++d) part[i].o[d] = {0.f, 0.f, 0.f, 0.f};
-    }
-    int unit = kNoScale;                             // the wave's value unit 2^unit
-
-    const int page_end = min(top / kPage + 1, (chunk + 1) * a.chunk_pages);
-    const int step = APART ? 1 : 4;
-    const int *table = a.set.tables + (int64_t)t.row * a.set.width;
-    for (int p = top < 0 ? page_end : chunk * a.chunk_pages + (APART ? 0 : wave); p < page_end; p += step) {
-        const int page = __builtin_amdgcn_readfirstlane(table[p]);
-        if (page < 0 || page >= a.layer.pages) {
-            if (a.layer.status && lane == 0) atomicOr(a.layer.status, TQ_KV_BAD_PAGE);
-            continue;
-        }
-        const int64_t tile = (int64_t)page * a.layer.heads + t.kvh;
-        const char *kp = a.layer.k + tile * (kPage * D);
-        const char *vp = a.layer.v + tile * (kPage * D);
-        const float ks = a.layer.ks[tile * 4 + g];
-        float vs = a.layer.vs[tile * 4 + g];
-        uint4 kc[4][D / 64], vc[DT];
-        const int krow = (16 * (n >> 2) + (n & 3)) * D + g * 16;
+    // what a page needs: its codes and the scales of the lane's block
+    const int *table = a.set.tables + (int64_t)row * a.set.width;
+    uint4 kc[4][D / 64], vc[DT];
+    const int krow = (16 * (n >> 2) + (n & 3)) * D + g * 16, vrow = (g * D + n) * 16;
+    int ahead = begin < end ? table[begin] : 0;      // page id of the next load
+    bool fits = false;
+    auto tile_of = [&](int page) {
+        fits = page >= 0 && page < a.layer.pages;
+        if (!fits && a.layer.status && lane == 0) atomicOr(a.layer.status, TQ_KV_BAD_PAGE);
+        return (int64_t)(fits ? page : 0) * a.layer.heads + kvh;
+    };
+    auto load_keys = [&](int64_t tile) {
+        const char *kp = a.layer.k + tile * (kPage * D) + krow;
 #pragma unroll
         for (int s = 0; s < 4; ++s)
 #pragma unroll
-            for (int u = 0; u < D / 64; ++u)
-                kc[s][u] = *reinterpret_cast<const uint4 *>(kp + krow + 4 * s * D + u * 64);
+            for (int u = 0; u < D / 64; ++u) kc[s][u] = *reinterpret_cast<const uint4 *>(kp + 4 * s * D + u * 64);
+    };
+    auto load_values = [&](int64_t tile) {
+        const char *vp = a.layer.v + tile * (kPage * D) + vrow;
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-            vc[d] = *reinterpret_cast<const uint4 *>(vp + (g * D + d * 16 + n) * 16);
+        for (int d = 0; d < DT; ++d) vc[d] = *reinterpret_cast<const uint4 *>(vp + d * 256);
+    };
+    int64_t tile = 0;
+    float ks = 0.f, vs = 0.f;
+    if (begin < end) {
+        tile = tile_of(__builtin_amdgcn_readfirstlane(ahead));
+        load_keys(tile);
+        ks = a.layer.ks[tile * 4 + g];
+        vs = a.layer.vs[tile * 4 + g];
+        load_values(tile);
+        if (begin + W < end) ahead = table[begin + W];
+    }
 
+    f16x8 q[NT][KS];
+    float factor[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        const int r = r0 + 16 * i + n;
+        const int e = load_queries<D>(a, r < rows, (int64_t)(first + token[i]) * a.qt + (int64_t)(kvh * a.group + min(r, last) % a.group) * a.qh, g, q[i]);
+        factor[i] = ldexpf(fabsf(a.scale2), -e);
+    }
+    float m[NT], mv[NT], l[NT];                      // maxima (log2 units) of scores and of scores with value scales; sum
+    f32x4 o[NT][DT];                                 // in units of 2^(mv - kUnit)
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        m[i] = mv[i] = -__builtin_inff();
+        l[i] = 0.f;
+        for (int d = 0; d < DT; ++d) o[i][d] = {0.f, 0.f, 0.f, 0.f};
+    }
+
+    for (int p = begin; p < end; p += W) {
         // S^T of the page
         f32x4 x[NT][4];
 #pragma unroll
@@ -203,57 +224,64 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendArgs a) {
                 }
             }
         }
+        const bool here = fits, more = p + W < end;
+        const float kscale = ks;
+        if (more) {                                  // the next page's keys
+            tile = tile_of(__builtin_amdgcn_readfirstlane(ahead));
+            load_keys(tile);
+            ks = a.layer.ks[tile * 4 + g];
+            if (p + 2 * W < end) ahead = table[p + 2 * W];
+        }
+        __builtin_amdgcn_sched_barrier(0);
         const int base = p * kPage + 16 * g;         // position of the lane's first token
+        float vlog = vs > 0.f ? __log2f(vs) : -__builtin_inff();
         // A page that holds the row's end may hold anything past it: those
         // codes and scales are taken out before they meet a zero weight.
-        if ((p + 1) * kPage > t.len) {
-            const int left = min(max(t.len - base, 0), 16);
-            if (left == 0) vs = 0.f;
+        if ((p + 1) * kPage > len || !here) {
+            const int left = here ? min(max(len - base, 0), 16) : 0;
+            if (left == 0) vlog = -__builtin_inff();
 #pragma unroll
             for (int d = 0; d < DT; ++d) vc[d] = keep_tokens(vc[d], left);
         }
-        // the value unit: a power of two above every scale so far
-        int ve;
-        frexpf(vs, &ve);
-        ve = vs > 0.f ? ve : kNoScale;
-        const int v01 = max(__builtin_amdgcn_readlane(ve, 0), __builtin_amdgcn_readlane(ve, 16));
-        const int v23 = max(__builtin_amdgcn_readlane(ve, 32), __builtin_amdgcn_readlane(ve, 48));
-        const int higher = max(unit, max(v01, v23));
-        const float lower = unit == kNoScale ? 0.f : ldexpf(1.f, unit - higher);
-        const float vn = ldexpf(vs, -higher);
-        const bool moved = higher > unit;
-        unit = higher;
+        const bool masked = (p + 1) * kPage - 1 > low || !here;
 
-        f16x8 w[NT][2];
+        f16x8 w[NT][2], wl[NT][2];
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
-            const float f = factor[i] * ks;
-            float y[16], big = -__builtin_inff();
+            // never 0, so that a masked score stays -inf (a NaN scale of an unused block goes too)
+            const float f = fmaxf(factor[i] * kscale, 0x1p-126f);
+            if (masked) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
+                for (int j = 0; j < 16; ++j)
+                    if (base + j > pos[i] || !here) x[i][j >> 2][j & 3] = -__builtin_inff();
+            }
+            float big = max3(x[i][0][0], x[i][0][1], x[i][0][2]);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float z = x[i][s][r] * f;
-                    if (base + 4 * s + r > pos[i]) z = -__builtin_inff();
-                    y[4 * s + r] = z;
-                    big = fmaxf(big, z);
-                }
-            const float m = fmaxf(part[i].m, max_of_groups(big));
-            const float mm = m == -__builtin_inff() ? 0.f : m;
-            const float alpha = __builtin_amdgcn_exp2f(part[i].m - mm);
+            for (int j = 3; j < 15; j += 2) big = max3(big, x[i][j >> 2][j & 3], x[i][(j + 1) >> 2][(j + 1) & 3]);
+            big = fmaxf(big, x[i][3][3]) * f;
+            const float top1 = max_of_groups(big), top2 = max_of_groups(big + vlog);
+            if (__any(top1 > m[i] + kLag || top2 > mv[i] + kLag)) {
+                const float m1 = fmaxf(m[i], top1), m2 = fmaxf(mv[i], top2);
+                l[i] *= m[i] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m[i] - m1);
+                const float back = mv[i] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(mv[i] - m2);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[i][d] *= back;
+                m[i] = m1;
+                mv[i] = m2;
+            }
+            const float m1 = m[i] == -__builtin_inff() ? 0.f : m[i], m2 = mv[i] == -__builtin_inff() ? 0.f : mv[i];
+            const float gain = __builtin_amdgcn_exp2f(fminf(vlog + (m1 - m2) + kUnit, 126.f));
             float sum = 0.f;
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                const float e = __builtin_amdgcn_exp2f(y[j] - mm);
+                const float e = __builtin_amdgcn_exp2f(scaled_less(x[i][j >> 2][j & 3], f, m1));
                 sum += e;
-                w[i][j >> 3][j & 7] = (_Float16)(e * vn * (float)(1 << kUnit));
+                const float y = e * gain;
+                const _Float16 hi = (_Float16)y;
+                w[i][j >> 3][j & 7] = hi;
+                wl[i][j >> 3][j & 7] = (_Float16)(y - (float)hi);
             }
-            part[i].l = part[i].l * alpha + sum;
-            if (moved || __any(m > part[i].m)) {
-                const float both = alpha * lower;
-                for (int d = 0; d < DT; ++d) part[i].o[d] *= both;
-            }
-            part[i].m = m;
+            l[i] += sum;
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
@@ -261,94 +289,75 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendArgs a) {
             to_half<FP8>(vc[d], &lo, &hi);
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
-                part[i].o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, w[i][0], part[i].o[d], 0, 0, 0);
-                part[i].o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, w[i][1], part[i].o[d], 0, 0, 0);
+                o[i][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, w[i][0], o[i][d], 0, 0, 0);
+                o[i][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, w[i][1], o[i][d], 0, 0, 0);
+                o[i][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, wl[i][0], o[i][d], 0, 0, 0);
+                o[i][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, wl[i][1], o[i][d], 0, 0, 0);
             }
         }
+        if (more) {                                  // and its values
+            load_values(tile);
+            vs = a.layer.vs[tile * 4 + g];
+        }
+        __builtin_amdgcn_sched_barrier(0);
     }
 
-    const float back = unit == kNoScale ? 0.f : ldexpf(1.f, unit - kUnit);
     constexpr int OS = D + 4;                        // LDS row, off the banks' period
-    float *lo = lds, *lm = lds + (APART ? 0 : 4 * RW * OS);
+    float *lm = lds + W * RT * OS;
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-        const float l = sum_of_groups(part[i].l), m = part[i].m;
-        if constexpr (!APART) {
-            for (int d = 0; d < DT; ++d) {
-                f32x4 o = part[i].o[d] * back;
-                *reinterpret_cast<f32x4 *>(lo + ((wave * RW + 16 * i + n) * OS + d * 16 + g * 4)) = o;
-            }
-            if (g == 0) {
-                lm[(wave * RW + 16 * i + n) * 2] = m;
-                lm[(wave * RW + 16 * i + n) * 2 + 1] = l;
-            }
-        } else {
-            const int r = t.r0 + 16 * i + n;
-            if (r >= rows) continue;
-            const int64_t at = (int64_t)(t.first + r / a.group) * a.heads + t.kvh * a.group + r % a.group;
-            if (a.chunks > 1) {
-                float *po = a.part + (at * a.chunks + chunk) * D;
-                for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4 *>(po + d * 16 + g * 4) = part[i].o[d] * back;
-                if (g == 0) {
-                    float *pm = a.part + ((int64_t)a.set.total * a.heads * a.chunks * D + (at * a.chunks + chunk) * 2);
-                    pm[0] = m;
-                    pm[1] = l;
-                }
-            } else {
-                const float inv = l > 0.f || l != l ? back / l : 0.f;
-                for (int d = 0; d < DT; ++d) {
-                    unsigned short h[4];
-                    for (int j = 0; j < 4; ++j) h[j] = float_bits16(part[i].o[d][j] * inv, a.bf16);
-                    uint2 u;
-                    __builtin_memcpy(&u, h, 8);
-                    *reinterpret_cast<uint2 *>(static_cast<unsigned short *>(a.out) + at * D + d * 16 + g * 4) = u;
-                }
-                if (a.lse && g == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * 0.69314718056f;
-            }
+        const float sum = sum_of_groups(l[i]);
+        // back to units of 2^m, which the waves and parts have in common with the sum
+        const float back = mv[i] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(mv[i] - m[i] - kUnit);
+        for (int d = 0; d < DT; ++d)
+            *reinterpret_cast<f32x4 *>(lds + ((wave * RT + 16 * i + n) * OS + d * 16 + g * 4)) = o[i][d] * back;
+        if (g == 0) {
+            lm[(wave * RT + 16 * i + n) * 2] = m[i];
+            lm[(wave * RT + 16 * i + n) * 2 + 1] = sum;
         }
     }
-    if constexpr (!APART) {
-        __syncthreads();
-        // four coordinates of a row per thread
-        for (int j = threadIdx.x; j < RW * (D / 4); j += 256) {
-            const int row = j / (D / 4), d = (j % (D / 4)) * 4, r = t.r0 + row;
-            if (r >= rows) continue;
-            float m = -__builtin_inff();
-            for (int w = 0; w < 4; ++w) m = fmaxf(m, lm[(w * RW + row) * 2]);
-            const float mm = m == -__builtin_inff() ? 0.f : m;
-            float l = 0.f;
-            f32x4 o = {0.f, 0.f, 0.f, 0.f};
-            for (int w = 0; w < 4; ++w) {
-                const float e = __builtin_amdgcn_exp2f(lm[(w * RW + row) * 2] - mm);
-                l += e * lm[(w * RW + row) * 2 + 1];
-                o += e * *reinterpret_cast<const f32x4 *>(lo + ((w * RW + row) * OS + d));
+    __syncthreads();
+    // four coordinates of a row per thread
+    for (int j = threadIdx.x; j < RT * (D / 4); j += 64 * W) {
+        const int tr = j / (D / 4), d = (j % (D / 4)) * 4, r = r0 + tr;
+        if (r >= rows) continue;
+        float mt = -__builtin_inff();
+        for (int w = 0; w < W; ++w) mt = fmaxf(mt, lm[(w * RT + tr) * 2]);
+        const float mm = mt == -__builtin_inff() ? 0.f : mt;
+        float sum = 0.f;
+        f32x4 ot = {0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < W; ++w) {
+            const float e = __builtin_amdgcn_exp2f(lm[(w * RT + tr) * 2] - mm);
+            sum += e * lm[(w * RT + tr) * 2 + 1];
+            ot += e * *reinterpret_cast<const f32x4 *>(lds + ((w * RT + tr) * OS + d));
+        }
+        const int64_t at = (int64_t)(first + r / a.group) * a.heads + kvh * a.group + r % a.group;
+        if (a.chunks > 1) {
+            *reinterpret_cast<f32x4 *>(a.part + (at * a.chunks + chunk) * D + d) = ot;
+            if (d == 0) {
+                float *pm = a.part + ((int64_t)a.set.total * a.heads * a.chunks * D + (at * a.chunks + chunk) * 2);
+                pm[0] = mt;
+                pm[1] = sum;
             }
-            const int64_t at = (int64_t)(t.first + r / a.group) * a.heads + t.kvh * a.group + r % a.group;
-            if (a.chunks > 1) {
-                *reinterpret_cast<f32x4 *>(a.part + (at * a.chunks + chunk) * D + d) = o;
-                if (d == 0) {
-                    float *pm = a.part + ((int64_t)a.set.total * a.heads * a.chunks * D + (at * a.chunks + chunk) * 2);
-                    pm[0] = m;
-                    pm[1] = l;
-                }
-            } else {
-                const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-                unsigned short h[4];
-                for (int k = 0; k < 4; ++k) h[k] = float_bits16(o[k] * inv, a.bf16);
-                uint2 u;
-                __builtin_memcpy(&u, h, 8);
-                *reinterpret_cast<uint2 *>(static_cast<unsigned short *>(a.out) + at * D + d) = u;
-                if (a.lse && d == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * 0.69314718056f;
-            }
+        } else {
+            const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+            unsigned short h[4];
+            for (int k = 0; k < 4; ++k) h[k] = float_bits16(ot[k] * inv, a.bf16);
+            uint2 u;
+            __builtin_memcpy(&u, h, 8);
+            *reinterpret_cast<uint2 *>(static_cast<unsigned short *>(a.out) + at * D + d) = u;
+            if (a.lse && d == 0) a.lse[at] = sum == 0.f ? -__builtin_inff() : (mt + __log2f(sum)) * 0.69314718056f;
         }
     }
 }
 
-// Joins the parts of a row: a wave per (token, head).
-template <int D>
+// Joins the parts of a (token, head): W waves, each takes every W-th part.
+template <int D, int W>
 __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
-    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
+    constexpr int N = D / 64;
+    __shared__ float lds[W > 1 ? W * (D + 1) : 1];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t at = W > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
     if (at >= (int64_t)a.set.total * a.heads) return;
     const int token = (int)(at / a.heads);
     int row = token, first = token, count = 1;
@@ -367,13 +376,23 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
     for (int c = lane; c < parts; c += 64) m = fmaxf(m, pm[2 * c]);
     for (int k = 32; k; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
     const float mm = m == -__builtin_inff() ? 0.f : m;
-    constexpr int N = D / 64;
     float l = 0.f, o[N];
     for (int j = 0; j < N; ++j) o[j] = 0.f;
-    for (int c = 0; c < parts; ++c) {
+#pragma unroll 4
+    for (int c = W > 1 ? wave : 0; c < parts; c += W) {
         const float e = __builtin_amdgcn_exp2f(pm[2 * c] - mm);
         l += e * pm[2 * c + 1];
         for (int j = 0; j < N; ++j) o[j] += e * po[(int64_t)c * D + j * 64 + lane];
+    }
+    if constexpr (W > 1) {
+        for (int j = 0; j < N; ++j) lds[wave * (D + 1) + j * 64 + lane] = o[j];
+        if (lane == 0) lds[wave * (D + 1) + D] = l;
+        __syncthreads();
+        if (wave > 0) return;
+        for (int w = 1; w < W; ++w) {
+            for (int j = 0; j < N; ++j) o[j] += lds[w * (D + 1) + j * 64 + lane];
+            l += lds[w * (D + 1) + D];
+        }
     }
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
     for (int j = 0; j < N; ++j)
@@ -381,29 +400,35 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
     if (a.lse && lane == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * 0.69314718056f;
 }
 
-template <int D, bool FP8, int NT, bool APART>
+template <int D, bool FP8, int NT, int W>
 hipError_t launch(const AttendArgs &a, hipStream_t stream) {
-    constexpr int RW = 16 * NT, RT = APART ? 4 * RW : RW;
-    const size_t lds = APART ? 0 : sizeof(float) * 4 * RW * (D + 4 + 2);
+    constexpr int RT = 16 * NT;
+    constexpr size_t lds = sizeof(float) * W * RT * (D + 4 + 2);
     if (lds > 65536) {
         static const hipError_t once = hipFuncSetAttribute(
-            reinterpret_cast<const void *>(attend_kernel<D, FP8, NT, APART>),
+            reinterpret_cast<const void *>(attend_kernel<D, FP8, NT, W>),
             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (once != hipSuccess) return once;
     }
     const int64_t slots = a.set.starts ? (int64_t)a.set.total * a.group / RT + a.set.rows
                                        : (int64_t)a.set.rows * ((a.group + RT - 1) / RT);
-    attend_kernel<D, FP8, NT, APART><<<dim3((unsigned)(slots * a.chunks), (unsigned)a.layer.heads), 256, lds, stream>>>(a);
+    attend_kernel<D, FP8, NT, W><<<dim3((unsigned)(slots * a.chunks), (unsigned)a.layer.heads), 64 * W, lds, stream>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.chunks == 1) return e;
-    join_kernel<D><<<(unsigned)(((int64_t)a.set.total * a.heads + 3) / 4), 256, 0, stream>>>(a);
+    const int64_t outs = (int64_t)a.set.total * a.heads;
+    // many parts of few results: four waves each
+    if (a.chunks > 8) join_kernel<D, 4><<<(unsigned)outs, 256, 0, stream>>>(a);
+    else join_kernel<D, 1><<<(unsigned)((outs + 3) / 4), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
 template <int D, bool FP8>
 hipError_t pick(const AttendArgs &a, const AttendPlan &p, hipStream_t stream) {
-    if (p.rows_apart) return launch<D, FP8, 2, true>(a, stream);
-    return p.tile == 16 ? launch<D, FP8, 1, false>(a, stream) : launch<D, FP8, 2, false>(a, stream);
+    if constexpr (D < 256) {   // at 256 neither fits the registers
+        if (p.waves == 8) return launch<D, FP8, 1, 8>(a, stream);
+        if (p.tile == 32) return launch<D, FP8, 2, 4>(a, stream);
+    }
+    return launch<D, FP8, 1, 4>(a, stream);
 }
 
 }  // namespace
@@ -415,15 +440,14 @@ AttendPlan attend_plan(int64_t n, int rows, int group, int kv_heads, int width, 
     const int pages = (int)((len + kPage - 1) / kPage);
     // query rows of one key head and table row, on average
     const int64_t mean = (n * group + rows - 1) / rows;
-    p.rows_apart = mean > 64;
-    p.tile = p.rows_apart ? 128 : mean > 16 ? 32 : 16;
+    p.tile = mean > 16 && D < 256 ? 32 : 16;
     const int64_t units = ((n * group) / p.tile + rows) * kv_heads;
-    const int64_t want = 2048;
-    int64_t chunks = (want + units - 1) / units;
-    int each = (int)((pages + chunks - 1) / chunks);
-    if (each < 4) each = 4;
-    p.chunk_pages = each;
-    p.chunks = pages > 0 ? (pages + each - 1) / each : 1;
+    p.waves = p.tile == 16 && D < 256 && pages <= WHOLE ? 8 : 4;
+    int64_t each = pages <= WHOLE ? pages : pages * units / WANT;
+    if (each < 8) each = 8;
+    if (each > 64) each = 64;
+    p.chunk_pages = (int)each;
+    p.chunks = pages > 0 ? (int)((pages + each - 1) / each) : 1;
     return p;
 }
 

@@ -66,6 +66,7 @@ __device__ inline void flag(int *status, int bit) {
 // Workspace: ints.
 struct Scratch {
     int *head;        // [4]: free pages found, pairs to copy, live pages
+    int *place;       // [n] a row's pair in the list of copies
     int *begin;       // [n] first of a row's or pair's places in fresh
     int *more;        // [n] pages it asks for; bit 30: the first one replaces a shared page
     int *from, *to;   // [m] pairs of pages to copy (from -1: none)
@@ -79,7 +80,8 @@ __host__ __device__ inline Scratch scratch(void *ws, int64_t pages, int64_t rows
     const int64_t m = rows > n ? rows : n, pairs = m > pages ? m : pages;
     Scratch s;
     s.head = static_cast<int *>(ws);
-    s.begin = s.head + 4;
+    s.place = s.head + 4;
+    s.begin = s.place + m;
     s.more = s.begin + m;
     s.from = s.more + m;
     s.to = s.from + pairs;
@@ -90,28 +92,25 @@ __host__ __device__ inline Scratch scratch(void *ws, int64_t pages, int64_t rows
 }
 
 // ------------------------------------------------------------------ copies
-// Copies pages from[i] -> to[i], i < count, in all layers: pieces of 16 KiB
-// of one store (16 bytes x 4 per thread in flight), the scales with the first.
+// Copies pages from[i] -> to[i], i < *count, in all layers: along y pieces of 16
+// KiB of one store of one layer (16 bytes x 4 per thread in flight), the
+// scales with the first.
 constexpr int kPiece = 16384;
 __global__ __launch_bounds__(256) void copy_pages_kernel(PagesArgs a, const int *from, const int *to,
-                                                         const int *device_count, int count) {
-    if (device_count) count = min(count, *device_count);
+                                                         const int *list_length) {
+    const int count = *list_length;
+    if ((int)blockIdx.x >= count) return;
     const int64_t store = (int64_t)a.cache.heads * kPage * a.D;   // bytes of a page in one store
     const int pieces = (int)((store + kPiece - 1) / kPiece);
-    const int64_t units = (int64_t)a.layers * count * 2 * pieces;
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int piece = (int)(u % pieces);
-        const int64_t v = u / pieces;
-        const int which = (int)(v & 1);
-        const int64_t w = v >> 1;
-        const int layer = (int)(w / count), i = (int)(w % count);
+    const int which = blockIdx.y & 1, piece = (int)(blockIdx.y >> 1) % pieces, layer = (int)(blockIdx.y >> 1) / pieces;
+    const int64_t base = (int64_t)layer * a.cache.pages;
+    char *codes = (which ? a.cache.v : a.cache.k) + (int64_t)piece * kPiece;
+    const int n = (int)(min(store - (int64_t)piece * kPiece, (int64_t)kPiece) / 16);
+    for (int i = blockIdx.x; i < count; i += gridDim.x) {
         const int src = from[i], dst = to[i];
         if (src < 0) continue;
-        const int64_t base = (int64_t)layer * a.cache.pages;
-        char *codes = which ? a.cache.v : a.cache.k;
-        const uint4 *s = reinterpret_cast<const uint4 *>(codes + (base + src) * store + (int64_t)piece * kPiece);
-        uint4 *d = reinterpret_cast<uint4 *>(codes + (base + dst) * store + (int64_t)piece * kPiece);
-        const int n = (int)(min(store - (int64_t)piece * kPiece, (int64_t)kPiece) / 16);
+        const uint4 *s = reinterpret_cast<const uint4 *>(codes + (base + src) * store);
+        uint4 *d = reinterpret_cast<uint4 *>(codes + (base + dst) * store);
         uint4 x[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -128,12 +127,13 @@ __global__ __launch_bounds__(256) void copy_pages_kernel(PagesArgs a, const int 
     }
 }
 
-void launch_copy(const PagesArgs &a, const int *from, const int *to, const int *device_count, int count,
-                 hipStream_t stream) {
+void launch_copy(const PagesArgs &a, const int *from, const int *to, const int *count, int most, hipStream_t stream) {
     const int64_t store = (int64_t)a.cache.heads * kPage * a.D;
-    const int64_t units = (int64_t)a.layers * count * 2 * ((store + kPiece - 1) / kPiece);
-    const int64_t most = 256 * 8;
-    copy_pages_kernel<<<(unsigned)(units < most ? units : most), 256, 0, stream>>>(a, from, to, device_count, count);
+    const int64_t along = 2 * (int64_t)a.layers * ((store + kPiece - 1) / kPiece);
+    // some 16 workgroups per compute unit, each with a share of the list
+    int64_t x = 4096 / along;
+    x = x < 1 ? 1 : x > most ? most : x;
+    copy_pages_kernel<<<dim3((unsigned)x, (unsigned)along), 256, 0, stream>>>(a, from, to, count);
 }
 
 // ------------------------------------------------------------------ resize
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(256) void shrink_kernel(PagesArgs a, const int *goa
 __global__ __launch_bounds__(kPlanThreads) void resize_plan_kernel(PagesArgs a, const int *goals) {
     __shared__ int lds[kPlanThreads / 64];
     const Scratch s = scratch(a.ws, a.pages, a.rows, 0);
-    int total = 0;
+    int total = 0, copies = 0;
     for (int base = 0; base < a.rows; base += kPlanThreads) {
         const int row = base + threadIdx.x;
         int more = 0;
@@ -187,9 +187,17 @@ __global__ __launch_bounds__(kPlanThreads) void resize_plan_kernel(PagesArgs a, 
             s.more[row] = more | (shared ? kCopied : 0);
         }
         total += all;
+        if (__syncthreads_or(shared)) {
+            const int place = copies + block_scan(shared, lds, &all);
+            if (shared) s.place[row] = place;
+            copies += all;
+        }
     }
     const int found = list_free(a.refs, a.pages, min(total, a.pages), s.fresh, lds);
-    if (threadIdx.x == 0) s.head[0] = found;
+    if (threadIdx.x == 0) {
+        s.head[0] = found;
+        s.head[1] = copies;
+    }
 }
 
 // A wave per row: takes its pages.
@@ -197,13 +205,15 @@ __global__ __launch_bounds__(256) void grow_kernel(PagesArgs a, const int *goals
     const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (row >= a.rows) return;
     const Scratch s = scratch(a.ws, a.pages, a.rows, 0);
-    if (lane == 0) s.from[row] = -1;
     const int len = min(max(a.lens[row], 0), a.width * kPage), goal = goals[row];
     if (goal <= len || goal > a.width * kPage) return;
     const bool shared = s.more[row] & kCopied;
     const int more = s.more[row] & ~kCopied, begin = s.begin[row];
     if (more > 0 && (int64_t)begin + more > s.head[0]) {
-        if (lane == 0) flag(a.cache.status, TQ_KV_FULL);
+        if (lane == 0) {
+            flag(a.cache.status, TQ_KV_FULL);
+            if (shared) s.from[s.place[row]] = -1;
+        }
         return;
     }
     int *table = a.tables + (int64_t)row * a.width;
@@ -211,8 +221,8 @@ __global__ __launch_bounds__(256) void grow_kernel(PagesArgs a, const int *goals
     if (shared && lane == 0) {
         const int old = table[first];
         atomicSub(&a.refs[old], 1);
-        s.from[row] = old;
-        s.to[row] = s.fresh[begin];
+        s.from[s.place[row]] = old;
+        s.to[s.place[row]] = s.fresh[begin];
     }
     for (int j = lane; j < more; j += 64) {
         const int page = s.fresh[begin + j];
@@ -241,13 +251,16 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(PagesArgs a, co
         int all;
         const int at = total + block_scan(part, lds, &all);
         if (i < n) {
-            s.begin[i] = at;
+            s.begin[i] = at;   // also the pair's place in the list of copies
             s.more[i] = part;
         }
         total += all;
     }
     const int found = list_free(a.refs, a.pages, min(total, a.pages), s.fresh, lds);
-    if (threadIdx.x == 0) s.head[0] = found;
+    if (threadIdx.x == 0) {
+        s.head[0] = found;
+        s.head[1] = total;
+    }
 }
 
 // A wave per pair: the new row into the workspace, before any row changes.
@@ -256,7 +269,6 @@ __global__ __launch_bounds__(256) void fork_stage_kernel(PagesArgs a, const int 
     if (i >= n) return;
     const Scratch s = scratch(a.ws, a.pages, a.rows, n);
     int from, to;
-    if (lane == 0) s.from[i] = -1;
     if (!pair_rows(a, src, dst, i, &from, &to)) return;
     const int len = min(max(a.lens[from], 0), a.width * kPage);
     const bool part = s.more[i], fits = !part || s.begin[i] < s.head[0];
@@ -266,12 +278,19 @@ __global__ __launch_bounds__(256) void fork_stage_kernel(PagesArgs a, const int 
     if (lane == 0) {
         s.slens[i] = fits ? len : 0;
         if (!fits) flag(a.cache.status, TQ_KV_FULL);
-        if (part && fits) {
-            const int old = table[whole], page = s.fresh[s.begin[i]];
-            s.stage[(int64_t)i * a.width + whole] = page;
-            if (old >= 0 && old < a.pages) s.from[i] = old;
-            else flag(a.cache.status, TQ_KV_BAD_PAGE);
-            s.to[i] = page;
+        if (part) {
+            int old = -1;
+            if (fits) {
+                const int page = s.fresh[s.begin[i]];
+                old = table[whole];
+                s.stage[(int64_t)i * a.width + whole] = page;
+                s.to[s.begin[i]] = page;
+                if (old < 0 || old >= a.pages) {
+                    old = -1;
+                    flag(a.cache.status, TQ_KV_BAD_PAGE);
+                }
+            }
+            s.from[s.begin[i]] = old;
         }
     }
 }
@@ -365,7 +384,7 @@ __global__ __launch_bounds__(256) void compact_apply_kernel(PagesArgs a) {
 
 size_t kv_rows_bytes(int64_t pages, int64_t rows, int64_t width, int64_t n) {
     const int64_t m = rows > n ? rows : n, pairs = m > pages ? m : pages;
-    return sizeof(int) * (size_t)(4 + 2 * m + 2 * pairs + pages + n + n * width);
+    return sizeof(int) * (size_t)(4 + 3 * m + 2 * pairs + pages + n + n * width);
 }
 
 hipError_t kv_resize(const PagesArgs &a, const int *goals, hipStream_t stream) {
@@ -374,7 +393,7 @@ hipError_t kv_resize(const PagesArgs &a, const int *goals, hipStream_t stream) {
     shrink_kernel<<<grid, 256, 0, stream>>>(a, goals);
     resize_plan_kernel<<<1, kPlanThreads, 0, stream>>>(a, goals);
     grow_kernel<<<grid, 256, 0, stream>>>(a, goals);
-    launch_copy(a, s.from, s.to, nullptr, a.rows, stream);
+    launch_copy(a, s.from, s.to, s.head + 1, a.rows, stream);
     return hipGetLastError();
 }
 
@@ -384,7 +403,7 @@ hipError_t kv_fork(const PagesArgs &a, const int *src, const int *dst, int n, hi
     fork_plan_kernel<<<1, kPlanThreads, 0, stream>>>(a, src, dst, n);
     fork_stage_kernel<<<grid, 256, 0, stream>>>(a, src, dst, n);
     fork_apply_kernel<<<grid, 256, 0, stream>>>(a, src, dst, n);
-    launch_copy(a, s.from, s.to, nullptr, n, stream);
+    launch_copy(a, s.from, s.to, s.head + 1, n, stream);
     return hipGetLastError();
 }
 

@@ -4,79 +4,94 @@ library.  Nothing in this file waits for the GPU except KVCache.check()."""
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 
 import torch
 
-from . import _shape, _stream
 from ._lib import (KV_BAD_PAGE, KV_BLOCK, KV_FULL, KV_NONFINITE, KV_PAGE, KV_TYPES, KVCacheView,
                    KVRowsView, RowsView, check, lib)
 
 _CODES = {"int8": torch.int8, "fp8": torch.float8_e4m3fn}
+_NAMES = {torch_type: name for name, torch_type in _CODES.items()}
 _FLOATS = {torch.float16: 0, torch.bfloat16: 1}
 _I32, _F32 = torch.int32, torch.float32
+_ref = ctypes.byref
+# the raw forms: what a call costs the host is a large part of a decoding step
+_stream_of = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
 
 
-def _on(t, dtype, name, device, ndim):
-    """The address of a contiguous tensor of this type on this device."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError("%s must be a CUDA (HIP) torch tensor" % name)
-    if t.dtype != dtype:
-        raise TypeError("%s must have dtype %s, got %s" % (name, dtype, t.dtype))
-    if t.dim() != ndim:
-        raise ValueError("%s must have %d dimensions" % (name, ndim))
-    if not t.is_contiguous():
+def _on(t, shape, dtype, index, name):
+    """The address of a contiguous tensor of this shape and type on GPU `index`."""
+    if not (isinstance(t, torch.Tensor) and t.shape == shape and t.dtype is dtype and t.get_device() == index
+            and t.is_contiguous()):
+        _refuse(t, shape, dtype, index, name)
         raise ValueError("%s must be contiguous" % name)
-    if t.device != device:
-        raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
     return t.data_ptr()
 
 
-def _device(t, name):
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError("%s must be a CUDA (HIP) torch tensor" % name)
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError("%s is on %s, which is not the current device" % (name, t.device))
-    return t.device
-
-
-def _packed(t, heads, d, name, device, dtype):
-    """tq_rows of packed vectors [n, heads, d]; strides are free except the last."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError("%s must be a CUDA (HIP) torch tensor" % name)
-    if t.dtype != dtype:
-        raise TypeError("%s must have dtype %s, got %s" % (name, dtype, t.dtype))
-    if t.device != device:
-        raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
-    if t.stride(2) != 1 and d > 1:
-        raise ValueError("%s: the last dimension must be contiguous" % name)
-    return RowsView(t.data_ptr(), t.stride(0), t.stride(1))
-
-
-def _rank3(t, name):
+def _refuse(t, shape, dtype, index, name):
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a CUDA (HIP) torch tensor" % name)
-    if t.dim() != 3:
-        raise ValueError("%s must have shape [tokens, heads, head_dim], got %s" % (name, tuple(t.shape)))
+    if t.shape != shape:
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if not t.is_cuda:
+        raise TypeError("%s must be a CUDA (HIP) torch tensor" % name)
+    if t.dtype is not dtype:
+        raise TypeError("%s must have dtype %s, got %s" % (name, dtype, t.dtype))
+    if t.get_device() != index:
+        raise ValueError("%s is on %s, not on GPU %d" % (name, t.device, index))
+
+
+def _packed(t, shape, dtype, index, name):
+    """tq_rows of packed vectors; strides are free except the last."""
+    if not (isinstance(t, torch.Tensor) and t.shape == shape and t.dtype is dtype and t.get_device() == index):
+        _refuse(t, shape, dtype, index, name)
+    a, b, c = t.stride()
+    if c != 1:
+        raise ValueError("%s: the last dimension must be contiguous" % name)
+    return RowsView(t.data_ptr(), a, b)
+
+
+def _dims(t, ndim, name):
+    """The shape of a tensor of so many dimensions."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a CUDA (HIP) torch tensor" % name)
+    shape = t.shape
+    if len(shape) != ndim:
+        raise ValueError("%s must have %d dimensions, got shape %s" % (name, ndim, tuple(shape)))
+    return shape
+
+
+def _gpu(t, name):
+    """The GPU of a call's tensors: the current one, where its kernels will run."""
+    index = t.get_device()
+    if index < 0:
+        raise TypeError("%s must be a CUDA (HIP) torch tensor" % name)
+    if index != _current_device():
+        raise ValueError("%s is on %s, which is not the current device" % (name, t.device))
+    return index
 
 
 def _float_type(t, name):
-    try:
-        return _FLOATS[t.dtype]
-    except KeyError:
-        raise TypeError("%s must be float16 or bfloat16, got %s" % (name, t.dtype)) from None
+    kind = _FLOATS.get(t.dtype)
+    if kind is None:
+        raise TypeError("%s must be float16 or bfloat16, got %s" % (name, t.dtype))
+    return kind
 
 
-def _results(q, out, return_lse):
-    """out and lse tensors of a call with queries q."""
-    n, heads, d = q.shape
+def _results(q, shape, index, out, return_lse):
+    """out and lse tensors of a call with queries q, and their addresses."""
     if out is None:
-        out = torch.empty((n, heads, d), dtype=q.dtype, device=q.device)
+        out = q.new_empty(shape)
+        at = out.data_ptr()
     else:
-        _shape(out, (n, heads, d), "out")
-        _on(out, q.dtype, "out", q.device, 3)
-    lse = torch.empty((n, heads), dtype=_F32, device=q.device) if return_lse else None
-    return out, lse
+        at = _on(out, shape, q.dtype, index, "out")
+    if not return_lse:
+        return out, None, at, None
+    lse = q.new_empty(shape[:2], dtype=_F32)
+    return out, lse, at, lse.data_ptr()
 
 
 def attention(q, k, v, starts, key_starts=None, *, causal=True, scale=None, longest=0, out=None,
@@ -92,30 +107,45 @@ def attention(q, k, v, starts, key_starts=None, *, causal=True, scale=None, long
     longest: the most queries of a row where the caller knows it.
     Returns out [n, heads, d], with return_lse also the float32 [n, heads]
     logarithm of each query's sum (-inf where it sees no key)."""
-    _rank3(q, "q")
-    _rank3(k, "k")
-    n, heads, d = q.shape
-    n_keys, kv_heads = k.shape[0], k.shape[1]
-    _shape(k, (n_keys, kv_heads, d), "k")
-    _shape(v, (n_keys, kv_heads, d), "v")
-    dev, dt = _device(q, "q"), _float_type(q, "q")
-    qv = _packed(q, heads, d, "q", dev, q.dtype)
-    kv = _packed(k, kv_heads, d, "k", dev, q.dtype)
-    vv = _packed(v, kv_heads, d, "v", dev, q.dtype)
-    at = _on(starts, _I32, "starts", dev, 1)
-    rows = starts.shape[0] - 1
+    shape = _dims(q, 3, "q")
+    n, heads, d = shape
+    keys = _dims(k, 3, "k")
+    n_keys, kv_heads, dk = keys
+    if dk != d:
+        raise ValueError("k must have head_dim %d, got %d" % (d, dk))
+    if _dims(v, 3, "v") != keys:
+        raise ValueError("v must have shape %s, got %s" % (tuple(keys), tuple(v.shape)))
+    index, dt = _gpu(q, "q"), _float_type(q, "q")
+    qv = _packed(q, shape, q.dtype, index, "q")
+    kv = _packed(k, keys, q.dtype, index, "k")
+    vv = _packed(v, keys, q.dtype, index, "v")
+    rows = _dims(starts, 1, "starts")[0] - 1
     if rows < 0:
         raise ValueError("starts must have rows + 1 entries")
-    kat = None
-    if key_starts is not None:
-        _shape(key_starts, (rows + 1,), "key_starts")
-        kat = _on(key_starts, _I32, "key_starts", dev, 1)
-    out, lse = _results(q, out, return_lse)
-    check(lib.tq_attention(ctypes.byref(qv), ctypes.byref(kv), ctypes.byref(vv), dt, n, n_keys,
-                           heads, kv_heads, d, at, kat, rows, longest, int(causal),
-                           1.0 / math.sqrt(d) if scale is None else scale, out.data_ptr(),
-                           lse.data_ptr() if return_lse else None, _stream(dev)))
+    at = _on(starts, (rows + 1,), _I32, index, "starts")
+    kat = None if key_starts is None else _on(key_starts, (rows + 1,), _I32, index, "key_starts")
+    out, lse, out_at, lse_at = _results(q, shape, index, out, return_lse)
+    check(lib.tq_attention(_ref(qv), _ref(kv), _ref(vv), dt, n, n_keys, heads, kv_heads, d, at, kat, rows,
+                           longest, 1 if causal else 0, 1.0 / math.sqrt(d) if scale is None else scale,
+                           out_at, lse_at, _stream_of(index)))
     return (out, lse) if return_lse else out
+
+
+@functools.lru_cache(maxsize=1024)
+def _attend_bytes(kv_heads, d, n, heads, width, rows, longest):
+    """Workspace of KVCache.attend: a function of sizes alone."""
+    view = KVCacheView(1 << 4, 1 << 4, 1, 1, None, 1, 1, kv_heads, d, 0)
+    need = ctypes.c_size_t()
+    check(lib.tq_kv_attend_workspace(_ref(view), n, heads, width, rows, longest, _ref(need)))
+    return need.value
+
+
+@functools.lru_cache(maxsize=1024)
+def _pages_bytes(pages, rows, width, n):
+    """Workspace of the calls of KVPages: a function of sizes alone."""
+    need = ctypes.c_size_t()
+    check(lib.tq_kv_rows_workspace(_ref(KVRowsView(None, None, None, pages, rows, width)), n, _ref(need)))
+    return need.value
 
 
 class KVCache:
@@ -149,29 +179,28 @@ class KVCache:
         return self
 
     def _adopt(self, k, v, k_scale, v_scale, status) -> None:
-        if not isinstance(k, torch.Tensor) or k.dim() != 5:
-            raise ValueError("k must be a tensor [layers, pages, kv_heads, 64, d]")
-        layers, pages, heads, page, d = k.shape
-        _shape(k, (layers, pages, heads, KV_PAGE, d), "k")
-        _shape(v, (layers, pages, heads, KV_PAGE // KV_BLOCK, d, KV_BLOCK), "v")
-        _shape(k_scale, (layers, pages, heads, KV_PAGE // KV_BLOCK), "k_scale")
-        _shape(v_scale, (layers, pages, heads, KV_PAGE // KV_BLOCK), "v_scale")
-        _shape(status, (1,), "status")
-        for name, dt in _CODES.items():
-            if k.dtype == dt:
-                self.dtype = name
-                break
-        else:
+        layers, pages, heads, page, d = shape = _dims(k, 5, "k")
+        name = _NAMES.get(k.dtype)
+        if name is None:
             raise TypeError("k must be int8 or float8_e4m3fn, got %s" % k.dtype)
-        dev = _device(k, "k")
+        if page != KV_PAGE:
+            raise ValueError("k must have shape [layers, pages, kv_heads, %d, d], got %s" % (KV_PAGE, tuple(shape)))
+        blocks = (layers, pages, heads, KV_PAGE // KV_BLOCK)
+        index = k.get_device()
+        self._view = KVCacheView(_on(k, shape, k.dtype, index, "k"),
+                                 _on(v, blocks + (d, KV_BLOCK), k.dtype, index, "v"),
+                                 _on(k_scale, blocks, _F32, index, "k_scale"),
+                                 _on(v_scale, blocks, _F32, index, "v_scale"),
+                                 None if status is None else _on(status, (1,), _I32, index, "status"),
+                                 pages, layers, heads, d, KV_TYPES[name])
+        _gpu(k, "k")
         self.k, self.v, self.k_scale, self.v_scale, self.status = k, v, k_scale, v_scale, status
-        self.layers, self.pages, self.kv_heads, self.head_dim, self.device = layers, pages, heads, d, dev
-        self._view = KVCacheView(_on(k, k.dtype, "k", dev, 5), _on(v, k.dtype, "v", dev, 6),
-                                 _on(k_scale, _F32, "k_scale", dev, 4),
-                                 _on(v_scale, _F32, "v_scale", dev, 4),
-                                 None if status is None else _on(status, _I32, "status", dev, 1),
-                                 pages, layers, heads, d, KV_TYPES[self.dtype])
-        self._ref = ctypes.byref(self._view)
+        self.layers, self.pages, self.kv_heads, self.head_dim, self.dtype = layers, pages, heads, d, name
+        self._index, self._ref = index, _ref(self._view)
+
+    @property
+    def device(self):
+        return self.k.device
 
     def check(self) -> None:
         """Waits for the GPU and raises RuntimeError for the conditions that
@@ -188,34 +217,31 @@ class KVCache:
             raise RuntimeError("; ".join(said))
 
     def _rows(self, tables, lens, starts, n):
-        rows = lens.shape[0]
-        if not isinstance(tables, torch.Tensor) or tables.dim() != 2:
-            raise ValueError("tables must be a tensor [rows, width]")
-        _shape(tables, (rows, tables.shape[1]), "tables")
+        if _current_device() != self._index:
+            raise ValueError("the cache is on GPU %d, which is not the current device" % self._index)
+        rows, width = shape = _dims(tables, 2, "tables")
         if starts is None:
             if n != rows:
                 raise ValueError("without starts there is one token per row: %d tokens, %d rows" % (n, rows))
+            at = None
         else:
-            _shape(starts, (rows + 1,), "starts")
-        return (_on(tables, _I32, "tables", self.device, 2), tables.shape[1],
-                _on(lens, _I32, "lens", self.device, 1),
-                None if starts is None else _on(starts, _I32, "starts", self.device, 1), rows)
+            at = _on(starts, (rows + 1,), _I32, self._index, "starts")
+        return (_on(tables, shape, _I32, self._index, "tables"), width,
+                _on(lens, (rows,), _I32, self._index, "lens"), at, rows)
 
     def append(self, layer: int, k, v, tables, lens, starts=None) -> None:
         """Quantises new tokens into one layer (tq_kv_append).  k, v: cuda
         float16 or bfloat16 [n, kv_heads, d], packed by rows, any strides with a contiguous
         last dimension.  tables int32 [rows, width], lens int32 [rows] (the
         new tokens included), starts int32 [rows + 1] (None: one per row)."""
-        _rank3(k, "k")
-        n = k.shape[0]
-        _shape(k, (n, self.kv_heads, self.head_dim), "k")
-        _shape(v, (n, self.kv_heads, self.head_dim), "v")
+        n = _dims(k, 3, "k")[0]
+        shape = (n, self.kv_heads, self.head_dim)
         dt = _float_type(k, "k")
-        kv = _packed(k, self.kv_heads, self.head_dim, "k", self.device, k.dtype)
-        vv = _packed(v, self.kv_heads, self.head_dim, "v", self.device, k.dtype)
+        kv = _packed(k, shape, k.dtype, self._index, "k")
+        vv = _packed(v, shape, k.dtype, self._index, "v")
         table, width, length, at, rows = self._rows(tables, lens, starts, n)
-        check(lib.tq_kv_append(self._ref, layer, ctypes.byref(kv), ctypes.byref(vv), dt, n, table, width,
-                               length, at, rows, _stream(self.device)))
+        check(lib.tq_kv_append(self._ref, layer, _ref(kv), _ref(vv), dt, n, table, width, length, at, rows,
+                               _stream_of(self._index)))
 
     def attend(self, layer: int, q, tables, lens, starts=None, *, scale=None, longest=0, out=None,
                return_lse=False, workspace=None):
@@ -228,25 +254,25 @@ class KVCache:
         workspace: a cuda uint8 tensor to use instead of a new one.
         Returns out [n, heads, d], with return_lse also the float32 [n, heads]
         logarithm of each query's sum (-inf, and out 0, for a row of length 0)."""
-        _rank3(q, "q")
-        n, heads, d = q.shape
-        _shape(q, (n, heads, self.head_dim), "q")
+        n, heads, d = shape = _dims(q, 3, "q")
+        if d != self.head_dim:
+            raise ValueError("q must have head_dim %d, got %d" % (self.head_dim, d))
         dt = _float_type(q, "q")
-        qv = _packed(q, heads, d, "q", self.device, q.dtype)
+        qv = _packed(q, shape, q.dtype, self._index, "q")
         table, width, length, at, rows = self._rows(tables, lens, starts, n)
-        need = ctypes.c_size_t()
-        check(lib.tq_kv_attend_workspace(self._ref, n, heads, width, rows, longest, ctypes.byref(need)))
-        if workspace is None:
-            if need.value:
-                workspace = torch.empty((need.value,), dtype=torch.uint8, device=self.device)
+        need = _attend_bytes(self.kv_heads, d, n, heads, width, rows, longest)
+        if workspace is not None:
+            ws = _on(workspace, workspace.shape, torch.uint8, self._index, "workspace")
+            need = workspace.numel()
+        elif need:
+            workspace = q.new_empty((need,), dtype=torch.uint8)
+            ws = workspace.data_ptr()
         else:
-            _on(workspace, torch.uint8, "workspace", self.device, 1)
-        out, lse = _results(q, out, return_lse)
-        check(lib.tq_kv_attend(self._ref, layer, ctypes.byref(qv), dt, n, heads, table, width, length, at,
-                               rows, longest, 1.0 / math.sqrt(d) if scale is None else scale,
-                               out.data_ptr(), lse.data_ptr() if return_lse else None,
-                               None if workspace is None else workspace.data_ptr(),
-                               0 if workspace is None else workspace.numel(), _stream(self.device)))
+            ws = None
+        out, lse, out_at, lse_at = _results(q, shape, self._index, out, return_lse)
+        check(lib.tq_kv_attend(self._ref, layer, _ref(qv), dt, n, heads, table, width, length, at, rows, longest,
+                               1.0 / math.sqrt(d) if scale is None else scale, out_at, lse_at, ws, need,
+                               _stream_of(self._index)))
         return (out, lse) if return_lse else out
 
 
@@ -268,48 +294,45 @@ class KVPages:
         return self
 
     def _adopt(self, tables, lens, refs) -> None:
-        if not isinstance(tables, torch.Tensor) or tables.dim() != 2:
-            raise ValueError("tables must be a tensor [rows, width]")
-        rows, width = tables.shape
-        _shape(lens, (rows,), "lens")
-        dev = _device(tables, "tables")
-        self.tables, self.lens, self.refs, self.device = tables, lens, refs, dev
-        self._view = KVRowsView(_on(tables, _I32, "tables", dev, 2), _on(lens, _I32, "lens", dev, 1),
-                                _on(refs, _I32, "refs", dev, 1), refs.shape[0], rows, width)
-        self._ref = ctypes.byref(self._view)
+        rows, width = shape = _dims(tables, 2, "tables")
+        pages = _dims(refs, 1, "refs")[0]
+        index = tables.get_device()
+        self._view = KVRowsView(_on(tables, shape, _I32, index, "tables"), _on(lens, (rows,), _I32, index, "lens"),
+                                _on(refs, (pages,), _I32, index, "refs"), pages, rows, width)
+        _gpu(tables, "tables")
+        self.tables, self.lens, self.refs = tables, lens, refs
+        self._index, self._ref = index, _ref(self._view)
 
-    def _workspace(self, n: int):
-        need = ctypes.c_size_t()
-        check(lib.tq_kv_rows_workspace(self._ref, n, ctypes.byref(need)))
-        return torch.empty((need.value,), dtype=torch.uint8, device=self.device)
+    def _workspace(self, n: int, cache):
+        if cache._index != self._index or _current_device() != self._index:
+            raise ValueError("the rows, the cache and the current device must be one GPU")
+        v = self._view
+        return self.lens.new_empty((_pages_bytes(v.pages, v.rows, v.width, n),), dtype=torch.uint8)
 
     def resize(self, goals, cache: KVCache) -> None:
         """Sets the rows' lengths to goals (int32 [rows], negative: leave):
         shrinking rows give pages back, growing ones take the lowest free
         pages in row order (tq_kv_resize).  A row that does not get its pages
         stays as it is, and cache.check() says so."""
-        _shape(goals, tuple(self.lens.shape), "goals")
-        at = _on(goals, _I32, "goals", self.device, 1)
-        ws = self._workspace(0)
-        check(lib.tq_kv_resize(self._ref, at, cache._ref, ws.data_ptr(), ws.numel(), _stream(self.device)))
+        at = _on(goals, self.lens.shape, _I32, self._index, "goals")
+        ws = self._workspace(0, cache)
+        check(lib.tq_kv_resize(self._ref, at, cache._ref, ws.data_ptr(), ws.numel(), _stream_of(self._index)))
 
     def fork(self, src, dst, cache: KVCache) -> None:
         """Makes rows dst (int32 [n], distinct) copies of rows src (int32
         [n]): whole pages are shared, a part-filled one is copied in every
         layer (tq_kv_fork)."""
-        if not isinstance(src, torch.Tensor) or src.dim() != 1:
-            raise ValueError("src must be a tensor [n]")
-        _shape(dst, tuple(src.shape), "dst")
-        a, b = _on(src, _I32, "src", self.device, 1), _on(dst, _I32, "dst", self.device, 1)
-        ws = self._workspace(src.shape[0])
-        check(lib.tq_kv_fork(self._ref, a, b, src.shape[0], cache._ref, ws.data_ptr(), ws.numel(),
-                             _stream(self.device)))
+        shape = _dims(src, 1, "src")
+        a, b = _on(src, shape, _I32, self._index, "src"), _on(dst, shape, _I32, self._index, "dst")
+        ws = self._workspace(shape[0], cache)
+        check(lib.tq_kv_fork(self._ref, a, b, shape[0], cache._ref, ws.data_ptr(), ws.numel(),
+                             _stream_of(self._index)))
 
     def compact(self, cache: KVCache):
         """Moves the live pages to the front of the pool and returns their
         number (cuda int32 [1]); the pages from there on are free (tq_kv_compact)."""
-        live = torch.empty(1, dtype=_I32, device=self.device)
-        ws = self._workspace(0)
+        live = self.lens.new_empty(1)
+        ws = self._workspace(0, cache)
         check(lib.tq_kv_compact(self._ref, cache._ref, live.data_ptr(), ws.data_ptr(), ws.numel(),
-                                _stream(self.device)))
+                                _stream_of(self._index)))
         return live

@@ -110,6 +110,21 @@ def test_large_scores_and_equal_ones():
     assert torch.all((out.double() - mean).abs() <= 2.0 ** -7 * (v.double().abs().max()))
 
 
+@pytest.mark.parametrize("size", [1e4, 1e8, 1e18])
+def test_scores_past_float32s_fractions(size):
+    # one key takes all, whatever the scores' rounding: the others are hundreds below
+    counts = [90]
+    q, k, v = (rows(counts, 1, 64, torch.bfloat16, 45 + s) for s in range(3))
+    out, lse = tq.attention(q * size, k, v, starts_of(counts), return_lse=True)
+    x = (q * size)[:, 0].double() @ k[:, 0].double().T
+    x.masked_fill_(torch.ones(90, 90, dtype=torch.bool, device="cuda").triu(1), -math.inf)
+    best = x.topk(2).values
+    sure = (best[:, 0] - best[:, 1] > 1e-5 * best[:, 0].abs() + 500)
+    assert sure.sum() > 60
+    assert torch.equal(out[sure, 0], v[x.argmax(1), 0][sure])
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+
+
 def test_repeats_are_equal_and_streams():
     counts = [300, 5, 211]
     q, k, v = (rows(counts, 8, 128, torch.bfloat16, 50 + s) for s in range(3))
