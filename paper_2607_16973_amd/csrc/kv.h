@@ -44,18 +44,23 @@ struct AttendArgs {
     int64_t qt, qh;
     void *out;
     float *lse;                   // or null
-    float *part;                  // [total * heads][chunks][D], then [..][2]; chunks > 1
+    int *info;                    // [units] first part and number of parts
+    float *parts;                 // [2 shares][tile][D + 4]: sums, maximum, weight
     float scale2;                 // scale * log2(e)
     int heads, group, bf16, wide;
-    int chunks, chunk_pages;      // the pages of a row in so many parts
+    int shares;
     int limit;                    // tokens of a row that are looked at
 };
-// How a call is split: query rows and waves per workgroup, pages per part.
+// How a call is split: query rows of a tile, tiles (units), waves that share
+// the units' pages.  line: a bound on the pages of all units.
 struct AttendPlan {
-    int tile, waves, chunks, chunk_pages;
+    int tile, shares;
+    bool join;
+    int64_t units, line;
 };
-AttendPlan attend_plan(int64_t n, int rows, int group, int kv_heads, int width, int longest, int D);
-size_t attend_part_bytes(const AttendPlan &p, int64_t n, int heads, int D);
+AttendPlan attend_plan(int64_t n, int rows, int group, int kv_heads, int width, int longest, int D, bool starts);
+size_t attend_info_bytes(const AttendPlan &p);
+size_t attend_bytes(const AttendPlan &p, int D);
 hipError_t kv_attend(const AttendArgs &a, const AttendPlan &p, int D, int type, hipStream_t stream);
 
 struct PromptArgs {

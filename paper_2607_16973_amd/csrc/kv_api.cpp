@@ -1,6 +1,7 @@
 // C ABI of the reader's calls: argument validation and dispatch.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <string>
@@ -169,8 +170,12 @@ tq_status tq_kv_attend_workspace(const tq_kv_cache *cache, int64_t n, int32_t he
         if ((st = heads_of(heads, cache->kv_heads)) != TQ_OK) return st;
         if (n < 0 || n > kMost || rows < 0 || width < 0 || longest < 0) return fail(TQ_EINVAL, "negative size");
         if (n == 0 || rows == 0) return TQ_OK;
-        const AttendPlan p = attend_plan(n, rows, heads / cache->kv_heads, cache->kv_heads, width, longest, cache->head_dim);
-        *bytes_out = attend_part_bytes(p, n, heads, cache->head_dim);
+        // rows of single tokens and rows of several (starts) may be cut differently
+        const int group = heads / cache->kv_heads;
+        for (const bool starts : {false, true}) {
+            const AttendPlan p = attend_plan(n, rows, group, cache->kv_heads, width, longest, cache->head_dim, starts);
+            *bytes_out = std::max(*bytes_out, attend_bytes(p, cache->head_dim));
+        }
         return TQ_OK;
     });
 }
@@ -189,12 +194,11 @@ tq_status tq_kv_attend(const tq_kv_cache *cache, int32_t layer, const tq_rows *q
         if (n == 0) return TQ_OK;
         if (!out || (reinterpret_cast<uintptr_t>(out) & 7)) return fail(TQ_EINVAL, "out is NULL or not 8-byte aligned");
         const int group = heads / cache->kv_heads;
-        const AttendPlan p = attend_plan(n, rows, group, cache->kv_heads, width, longest, cache->head_dim);
-        const size_t need = attend_part_bytes(p, n, heads, cache->head_dim);
-        if (need && (!ws || ws_bytes < need || !aligned16(ws))) return fail(TQ_EINVAL, "workspace too small or not aligned");
-        if ((n * group / p.tile + (int64_t)rows * ((group + p.tile - 1) / p.tile)) * p.chunks >= kMostGroups ||
-            n * heads >= kMostGroups || n * group > kMost)
-            return fail(TQ_EUNSUPPORTED, "too many queries for one call");
+        const AttendPlan p = attend_plan(n, rows, group, cache->kv_heads, width, longest, cache->head_dim, starts != nullptr);
+        if (!ws || ws_bytes < attend_bytes(p, cache->head_dim) || !aligned16(ws))
+            return fail(TQ_EINVAL, "workspace too small or not aligned");
+        if (p.line > kMost || n * heads >= kMostGroups || n * group > kMost)
+            return fail(TQ_EUNSUPPORTED, "too many queries or tokens for one call");
         if ((st = device_ready()) != TQ_OK) return st;
         AttendArgs a;
         a.layer = layer_of(cache, layer);
@@ -203,14 +207,14 @@ tq_status tq_kv_attend(const tq_kv_cache *cache, int32_t layer, const tq_rows *q
         a.qt = q->token_stride, a.qh = q->head_stride;
         a.out = out;
         a.lse = lse;
-        a.part = static_cast<float *>(ws);
+        a.info = static_cast<int *>(ws);
+        a.parts = reinterpret_cast<float *>(static_cast<char *>(ws) + attend_info_bytes(p));
         a.scale2 = scale * 1.44269504089f;
         a.heads = heads;
         a.group = group;
         a.bf16 = dtype == TQ_BF16;
         a.wide = wide_rows(q);
-        a.chunks = p.chunks;
-        a.chunk_pages = p.chunk_pages;
+        a.shares = p.shares;
         a.limit = longest > 0 && longest < width * kPage ? longest : width * kPage;
         const hipError_t e = kv_attend(a, p, cache->head_dim, cache->type, static_cast<hipStream_t>(stream));
         return e == hipSuccess ? TQ_OK : hip_fail(e, "attention over the cache");

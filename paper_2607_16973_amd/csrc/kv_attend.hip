@@ -28,11 +28,6 @@
 namespace tq {
 namespace {
 
-#ifndef WANT
-#define WANT 4096
-#define WHOLE 32
-#endif
-
 constexpr float kUnit = 6.f;      // weights are held in units of 2^-kUnit ...
 constexpr float kLag = 8.f;       // ... and may pass the running maximum by 2^kLag before it follows
 
@@ -111,61 +106,127 @@ __device__ inline int load_queries(const AttendArgs &a, bool in, int64_t at, int
     return e;
 }
 
-// Rows of few queries (decoding, drafted tokens): NT tiles of 16 query rows that
-// the W waves of the workgroup share.  Each wave takes every W-th page and
-// has the next one's codes on the way while it works; the waves are joined
-// through LDS.  Bound by the memory system: 16 pages of 64 D bytes in
-// flight per compute unit.
-template <int D, bool FP8, int NT, int W>
-__global__ __launch_bounds__(64 * W) void attend_kernel(AttendArgs a) {
+// Rows of few queries (decoding, drafted tokens).  A unit is a tile of 16 NT
+// query rows of one key head of one table row, and has that row's pages to
+// go through.  All units' pages form one line, which is cut into equal
+// shares, one per wave of the grid: rows of very different lengths load the
+// machine evenly, and a wave has the next page's codes on the way while it
+// works, across units too.  A unit that lies in one share is written out at
+// once; of the others each share leaves a part (at most two per wave: at
+// its begin and at its end) for join_kernel.  Bound by the memory system:
+// up to 16 pages of 64 D bytes in flight per compute unit.
+struct Place {                       // a page of the line; the same in all lanes
+    int row, tile, kvh, page;        // page of the row
+    int tiles, pages;                // of the row
+    int len, count, first;
+};
+
+// Tiles and pages of a table row.  A row without tokens has one page, which
+// nobody sees.
+template <int RT>
+__device__ inline void row_shape(const AttendArgs &a, int row, Place *p) {
+    row_tokens(a.set.starts, row, a.set.total, &p->first, &p->count);
+    p->len = a.set.lens[row];
+    p->tiles = (p->count * a.group + RT - 1) / RT;
+    p->pages = max((min(p->len, a.limit) + kPage - 1) / kPage, 1);
+}
+
+template <int RT>
+__device__ inline void to_row(const AttendArgs &a, int row, Place *p) {
+    p->row = row;
+    row_shape<RT>(a, row, p);
+    p->len = __builtin_amdgcn_readfirstlane(p->len);
+    p->count = __builtin_amdgcn_readfirstlane(p->count);
+    p->first = __builtin_amdgcn_readfirstlane(p->first);
+    p->tiles = __builtin_amdgcn_readfirstlane(p->tiles);
+    p->pages = __builtin_amdgcn_readfirstlane(p->pages);
+}
+
+template <int RT>
+__device__ inline void advance(const AttendArgs &a, Place *p) {
+    if (++p->page < p->pages) return;
+    p->page = 0;
+    if (++p->kvh < a.layer.heads) return;
+    p->kvh = 0;
+    if (++p->tile < p->tiles) return;
+    p->tile = 0;
+    int row = p->row;
+    do {
+        if (++row >= a.set.rows) return;             // past the line: never used
+        to_row<RT>(a, row, p);
+    } while (p->tiles == 0);
+}
+
+// The number of a unit in the list of parts (first: the row's first token,
+// which row_tokens keeps inside the call, and the number with it).
+template <int RT>
+__device__ inline int64_t unit_of(const AttendArgs &a, int row, int first, int tile, int kvh) {
+    const int64_t slot = a.set.starts ? (int64_t)first * a.group / RT + row : (int64_t)row * ((a.group + RT - 1) / RT);
+    return (slot + tile) * a.layer.heads + kvh;
+}
+
+template <int D, bool FP8, int NT>
+__global__ __launch_bounds__(256) void attend_kernel(AttendArgs a) {
     constexpr int KS = D / 32;                       // 32-wide steps of the first product
     constexpr int DT = D / 16;
-    constexpr int RT = 16 * NT;                      // rows of the workgroup
-    extern __shared__ __align__(16) float lds[];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int n = lane & 15, g = lane >> 4;
+    constexpr int RT = 16 * NT;
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int share = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    const int heads = a.layer.heads;
 
-    int64_t slot = blockIdx.x / a.chunks;
-    const int chunk = blockIdx.x % a.chunks, kvh = blockIdx.y;
-    int row, first, count;
-    if (a.set.starts) {
-        row = slot_row(a.set.starts, a.set.rows, slot, a.group, RT, 1);
-        slot -= slot_begin(a.set.starts, row, a.group, RT, 1);
-    } else {   // one token per row: its group in ceil(group / RT) tiles
-        const int per = (a.group + RT - 1) / RT;
-        row = (int)(slot / per);
-        slot %= per;
+    // the line's length, the wave's share [x, end) and where x lies
+    auto pages_at = [&](int row) {
+        Place p;
+        if (row >= a.set.rows) return 0;
+        row_shape<RT>(a, row, &p);
+        return p.tiles * p.pages * heads;
+    };
+    auto running = [&](int v) {                      // inclusive sum over the lanes
+        for (int k = 1; k < 64; k <<= 1) {
+            const int y = __shfl_up(v, k);
+            if (lane >= k) v += y;
+        }
+        return v;
+    };
+    int total = 0, sums = 0;
+    for (int base = 0; base < a.set.rows; base += 64) {
+        sums = running(pages_at(base + lane));
+        total += __builtin_amdgcn_readlane(sums, 63);
     }
-    row_tokens(a.set.starts, row, a.set.total, &first, &count);
-    const int rows = count * a.group;
-    if (slot < 0 || slot * RT >= rows) return;       // the whole workgroup
-    const int r0 = (int)slot * RT;
-    const int true_len = a.set.lens[row];
-    const int len = min(true_len, a.limit);
-
-    // positions: the last key that each row, any row and every row sees
-    int pos[NT], token[NT];
-    const int last = min(rows - 1, r0 + RT - 1);
-    const int top = min(true_len - count + last / a.group, len - 1);
-    const int low = min(true_len - count + r0 / a.group, len - 1);
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        token[i] = min(r0 + 16 * i + n, last) / a.group;
-        pos[i] = min(true_len - count + token[i], len - 1);
+    const int each = (total + a.shares - 1) / a.shares;
+    const int x = share * each, end = min(x + each, total);
+    if (x >= end) return;
+    Place cur;
+    {
+        int before = 0;
+        for (int base = 0;; base += 64) {
+            if (a.set.rows > 64) sums = running(pages_at(base + lane));
+            const uint64_t past = __ballot(before + sums > x);
+            if (past) {
+                const int at = __builtin_ctzll(past);
+                if (at) before += __builtin_amdgcn_readlane(sums, at - 1);
+                to_row<RT>(a, base + at, &cur);
+                break;
+            }
+            before += __builtin_amdgcn_readlane(sums, 63);
+        }
+        const int within = x - before, unit = within / cur.pages;
+        cur.page = within % cur.pages;
+        cur.tile = unit / heads;
+        cur.kvh = unit % heads;
     }
-    const int begin = chunk * a.chunk_pages + wave;
-    const int end = top < 0 ? 0 : min(top / kPage + 1, (chunk + 1) * a.chunk_pages);
 
     // what a page needs: its codes and the scales of the lane's block
-    const int *table = a.set.tables + (int64_t)row * a.set.width;
     uint4 kc[4][D / 64], vc[DT];
     const int krow = (16 * (n >> 2) + (n & 3)) * D + g * 16, vrow = (g * D + n) * 16;
-    int ahead = begin < end ? table[begin] : 0;      // page id of the next load
+    auto any_in = [&](const Place &p) { return p.page * kPage < min(p.len, a.limit); };
+    auto id_of = [&](const Place &p) { return any_in(p) ? a.set.tables[(int64_t)p.row * a.set.width + p.page] : -1; };
     bool fits = false;
-    auto tile_of = [&](int page) {
-        fits = page >= 0 && page < a.layer.pages;
-        if (!fits && a.layer.status && lane == 0) atomicOr(a.layer.status, TQ_KV_BAD_PAGE);
-        return (int64_t)(fits ? page : 0) * a.layer.heads + kvh;
+    auto tile_of = [&](const Place &p, int page) {
+        const bool in = page >= 0 && page < a.layer.pages, any = any_in(p);
+        fits = in && any;
+        if (!in && any && a.layer.status && lane == 0) atomicOr(a.layer.status, TQ_KV_BAD_PAGE);
+        return (int64_t)(fits ? page : 0) * heads + p.kvh;
     };
     auto load_keys = [&](int64_t tile) {
         const char *kp = a.layer.k + tile * (kPage * D) + krow;
@@ -179,71 +240,86 @@ __global__ __launch_bounds__(64 * W) void attend_kernel(AttendArgs a) {
 #pragma unroll
         for (int d = 0; d < DT; ++d) vc[d] = *reinterpret_cast<const uint4 *>(vp + d * 256);
     };
-    int64_t tile = 0;
-    float ks = 0.f, vs = 0.f;
-    if (begin < end) {
-        tile = tile_of(__builtin_amdgcn_readfirstlane(ahead));
-        load_keys(tile);
-        ks = a.layer.ks[tile * 4 + g];
-        vs = a.layer.vs[tile * 4 + g];
-        load_values(tile);
-        if (begin + W < end) ahead = table[begin + W];
+    int64_t tile = tile_of(cur, __builtin_amdgcn_readfirstlane(id_of(cur)));
+    load_keys(tile);
+    float ks = a.layer.ks[tile * 4 + g], vs = a.layer.vs[tile * 4 + g];
+    load_values(tile);
+    Place next = cur;                                // the page whose codes come next, its id on the way
+    int ahead = 0;
+    if (x + 1 < end) {
+        advance<RT>(a, &next);
+        ahead = id_of(next);
     }
 
     f16x8 q[NT][KS];
     float factor[NT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        const int r = r0 + 16 * i + n;
-        const int e = load_queries<D>(a, r < rows, (int64_t)(first + token[i]) * a.qt + (int64_t)(kvh * a.group + min(r, last) % a.group) * a.qh, g, q[i]);
-        factor[i] = ldexpf(fabsf(a.scale2), -e);
-    }
+    int pos[NT];                                     // the last key a row sees
+    int top = -1, low = -1;                          // the last one any row and every row sees
     float m[NT], mv[NT], l[NT];                      // maxima (log2 units) of scores and of scores with value scales; sum
     f32x4 o[NT][DT];                                 // in units of 2^(mv - kUnit)
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        m[i] = mv[i] = -__builtin_inff();
-        l[i] = 0.f;
-        for (int d = 0; d < DT; ++d) o[i][d] = {0.f, 0.f, 0.f, 0.f};
-    }
+    int from = cur.page;                             // the first page of the unit in this share
+    bool open = true;                                // a unit begins
 
-    for (int p = begin; p < end; p += W) {
-        // S^T of the page
-        f32x4 x[NT][4];
+    for (int at = x; at < end; ++at) {
+        const int len = min(cur.len, a.limit);
+        const int rows = cur.count * a.group, r0 = cur.tile * RT, last = min(rows - 1, r0 + RT - 1);
+        if (open) {
+            from = cur.page;
+            top = min(cur.len - cur.count + last / a.group, len - 1);
+            low = min(cur.len - cur.count + r0 / a.group, len - 1);
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            for (int i = 0; i < NT; ++i) x[i][s] = {0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < NT; ++i) {
+                const int r = min(r0 + 16 * i + n, last), token = r / a.group;
+                pos[i] = min(cur.len - cur.count + token, len - 1);
+                const int e = load_queries<D>(a, r0 + 16 * i + n <= last,
+                                              (int64_t)(cur.first + token) * a.qt + (int64_t)(cur.kvh * a.group + r % a.group) * a.qh, g, q[i]);
+                factor[i] = ldexpf(fabsf(a.scale2), -e);
+                m[i] = mv[i] = -__builtin_inff();
+                l[i] = 0.f;
+                for (int d = 0; d < DT; ++d) o[i][d] = {0.f, 0.f, 0.f, 0.f};
+            }
+            open = false;
+        }
+        // S^T of the page
+        f32x4 s[NT][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            for (int i = 0; i < NT; ++i) s[i][j] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int u = 0; u < D / 64; ++u) {
                 f16x8 lo, hi;
-                to_half<FP8>(kc[s][u], &lo, &hi);
+                to_half<FP8>(kc[j][u], &lo, &hi);
 #pragma unroll
                 for (int i = 0; i < NT; ++i) {
-                    x[i][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, q[i][2 * u], x[i][s], 0, 0, 0);
-                    x[i][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, q[i][2 * u + 1], x[i][s], 0, 0, 0);
+                    s[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, q[i][2 * u], s[i][j], 0, 0, 0);
+                    s[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, q[i][2 * u + 1], s[i][j], 0, 0, 0);
                 }
             }
         }
-        const bool here = fits, more = p + W < end;
+        const bool here = fits, more = at + 1 < end;
         const float kscale = ks;
-        if (more) {                                  // the next page's keys
-            tile = tile_of(__builtin_amdgcn_readfirstlane(ahead));
+        const Place then = next;                     // the next page's keys
+        if (more) {
+            tile = tile_of(next, __builtin_amdgcn_readfirstlane(ahead));
             load_keys(tile);
             ks = a.layer.ks[tile * 4 + g];
-            if (p + 2 * W < end) ahead = table[p + 2 * W];
+            if (at + 2 < end) {
+                advance<RT>(a, &next);
+                ahead = id_of(next);
+            }
         }
         __builtin_amdgcn_sched_barrier(0);
-        const int base = p * kPage + 16 * g;         // position of the lane's first token
+        const int base = cur.page * kPage + 16 * g;  // position of the lane's first token
         float vlog = vs > 0.f ? __log2f(vs) : -__builtin_inff();
         // A page that holds the row's end may hold anything past it: those
         // codes and scales are taken out before they meet a zero weight.
-        if ((p + 1) * kPage > len || !here) {
+        if ((cur.page + 1) * kPage > len || !here) {
             const int left = here ? min(max(len - base, 0), 16) : 0;
             if (left == 0) vlog = -__builtin_inff();
 #pragma unroll
             for (int d = 0; d < DT; ++d) vc[d] = keep_tokens(vc[d], left);
         }
-        const bool masked = (p + 1) * kPage - 1 > low || !here;
+        const bool masked = (cur.page + 1) * kPage - 1 > low || !here;
 
         f16x8 w[NT][2], wl[NT][2];
 #pragma unroll
@@ -253,12 +329,12 @@ __global__ __launch_bounds__(64 * W) void attend_kernel(AttendArgs a) {
             if (masked) {
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
-                    if (base + j > pos[i] || !here) x[i][j >> 2][j & 3] = -__builtin_inff();
+                    if (base + j > pos[i] || !here) s[i][j >> 2][j & 3] = -__builtin_inff();
             }
-            float big = max3(x[i][0][0], x[i][0][1], x[i][0][2]);
+            float big = max3(s[i][0][0], s[i][0][1], s[i][0][2]);
 #pragma unroll
-            for (int j = 3; j < 15; j += 2) big = max3(big, x[i][j >> 2][j & 3], x[i][(j + 1) >> 2][(j + 1) & 3]);
-            big = fmaxf(big, x[i][3][3]) * f;
+            for (int j = 3; j < 15; j += 2) big = max3(big, s[i][j >> 2][j & 3], s[i][(j + 1) >> 2][(j + 1) & 3]);
+            big = fmaxf(big, s[i][3][3]) * f;
             const float top1 = max_of_groups(big), top2 = max_of_groups(big + vlog);
             if (__any(top1 > m[i] + kLag || top2 > mv[i] + kLag)) {
                 const float m1 = fmaxf(m[i], top1), m2 = fmaxf(mv[i], top2);
@@ -274,7 +350,7 @@ __global__ __launch_bounds__(64 * W) void attend_kernel(AttendArgs a) {
             float sum = 0.f;
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                const float e = __builtin_amdgcn_exp2f(scaled_less(x[i][j >> 2][j & 3], f, m1));
+                const float e = __builtin_amdgcn_exp2f(scaled_less(s[i][j >> 2][j & 3], f, m1));
                 sum += e;
                 const float y = e * gain;
                 const _Float16 hi = (_Float16)y;
@@ -300,89 +376,90 @@ __global__ __launch_bounds__(64 * W) void attend_kernel(AttendArgs a) {
             vs = a.layer.vs[tile * 4 + g];
         }
         __builtin_amdgcn_sched_barrier(0);
-    }
 
-    constexpr int OS = D + 4;                        // LDS row, off the banks' period
-    float *lm = lds + W * RT * OS;
+        if (cur.page + 1 == cur.pages || !more) {    // the unit, or the share, ends here
+            const bool whole = from == 0 && cur.page + 1 == cur.pages;
+            const int place = 2 * share + (at - x == cur.page - from ? 0 : 1);   // the share's first unit, or its last
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        const float sum = sum_of_groups(l[i]);
-        // back to units of 2^m, which the waves and parts have in common with the sum
-        const float back = mv[i] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(mv[i] - m[i] - kUnit);
-        for (int d = 0; d < DT; ++d)
-            *reinterpret_cast<f32x4 *>(lds + ((wave * RT + 16 * i + n) * OS + d * 16 + g * 4)) = o[i][d] * back;
-        if (g == 0) {
-            lm[(wave * RT + 16 * i + n) * 2] = m[i];
-            lm[(wave * RT + 16 * i + n) * 2 + 1] = sum;
-        }
-    }
-    __syncthreads();
-    // four coordinates of a row per thread
-    for (int j = threadIdx.x; j < RT * (D / 4); j += 64 * W) {
-        const int tr = j / (D / 4), d = (j % (D / 4)) * 4, r = r0 + tr;
-        if (r >= rows) continue;
-        float mt = -__builtin_inff();
-        for (int w = 0; w < W; ++w) mt = fmaxf(mt, lm[(w * RT + tr) * 2]);
-        const float mm = mt == -__builtin_inff() ? 0.f : mt;
-        float sum = 0.f;
-        f32x4 ot = {0.f, 0.f, 0.f, 0.f};
-        for (int w = 0; w < W; ++w) {
-            const float e = __builtin_amdgcn_exp2f(lm[(w * RT + tr) * 2] - mm);
-            sum += e * lm[(w * RT + tr) * 2 + 1];
-            ot += e * *reinterpret_cast<const f32x4 *>(lds + ((w * RT + tr) * OS + d));
-        }
-        const int64_t at = (int64_t)(first + r / a.group) * a.heads + kvh * a.group + r % a.group;
-        if (a.chunks > 1) {
-            *reinterpret_cast<f32x4 *>(a.part + (at * a.chunks + chunk) * D + d) = ot;
-            if (d == 0) {
-                float *pm = a.part + ((int64_t)a.set.total * a.heads * a.chunks * D + (at * a.chunks + chunk) * 2);
-                pm[0] = mt;
-                pm[1] = sum;
+            for (int i = 0; i < NT; ++i) {
+                const float sum = sum_of_groups(l[i]);
+                // to units of 2^m, which the parts have in common with the sum
+                const float back = mv[i] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(mv[i] - m[i] - kUnit);
+                const int r = r0 + 16 * i + n;
+                if (r <= last) {
+                    if (whole) {
+                        const int64_t to = (int64_t)(cur.first + r / a.group) * a.heads + cur.kvh * a.group + r % a.group;
+                        const float inv = sum > 0.f || sum != sum ? back / sum : 0.f;
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) {
+                            unsigned short h[4];
+                            for (int k = 0; k < 4; ++k) h[k] = float_bits16(o[i][d][k] * inv, a.bf16);
+                            uint2 u;
+                            __builtin_memcpy(&u, h, 8);
+                            *reinterpret_cast<uint2 *>(static_cast<unsigned short *>(a.out) + to * D + d * 16 + g * 4) = u;
+                        }
+                        if (a.lse && g == 0) a.lse[to] = sum == 0.f ? -__builtin_inff() : (m[i] + __log2f(sum)) * 0.69314718056f;
+                    } else {
+                        float *po = a.parts + ((int64_t)place * RT + 16 * i + n) * (D + 4);
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4 *>(po + d * 16 + g * 4) = o[i][d] * back;
+                        if (g == 0) {
+                            po[D] = m[i];
+                            po[D + 1] = sum;
+                        }
+                    }
+                }
             }
-        } else {
-            const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-            unsigned short h[4];
-            for (int k = 0; k < 4; ++k) h[k] = float_bits16(ot[k] * inv, a.bf16);
-            uint2 u;
-            __builtin_memcpy(&u, h, 8);
-            *reinterpret_cast<uint2 *>(static_cast<unsigned short *>(a.out) + at * D + d) = u;
-            if (a.lse && d == 0) a.lse[at] = sum == 0.f ? -__builtin_inff() : (mt + __log2f(sum)) * 0.69314718056f;
+            // who begins a unit says where its parts are
+            if (from == 0 && lane == 0) {
+                const int begin = at - cur.page, finish = begin + cur.pages - 1;   // in the line
+                reinterpret_cast<int2 *>(a.info)[unit_of<RT>(a, cur.row, cur.first, cur.tile, cur.kvh)] =
+                    make_int2(place, finish / each - begin / each + 1);
+            }
+            open = true;
         }
+        cur = then;
     }
 }
 
-// Joins the parts of a (token, head): W waves, each takes every W-th part.
-template <int D, int W>
+// Joins the parts of a (token, head) whose unit several shares have: W waves,
+// each takes every W-th part.
+template <int D, int RT, int W>
 __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
     constexpr int N = D / 64;
     __shared__ float lds[W > 1 ? W * (D + 1) : 1];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int64_t at = W > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
     if (at >= (int64_t)a.set.total * a.heads) return;
-    const int token = (int)(at / a.heads);
+    const int token = (int)(at / a.heads), head = (int)(at % a.heads);
     int row = token, first = token, count = 1;
     if (a.set.starts) {
         row = slot_row(a.set.starts, a.set.rows, token, 1, 1, 0);
         row_tokens(a.set.starts, row, a.set.total, &first, &count);
+        if (token < first || token >= first + count) return;
     }
-    const int true_len = a.set.lens[row];
-    const int len = min(true_len, a.limit);
-    const int pos = min(true_len - count + (token - first), len - 1);
-    // parts that hold tokens this query sees
-    const int parts = pos < 0 ? 0 : pos / (a.chunk_pages * kPage) + 1;
-    const float *po = a.part + at * a.chunks * D;
-    const float *pm = a.part + ((int64_t)a.set.total * a.heads * D + at * 2) * a.chunks;
+    const int r = (token - first) * a.group + head % a.group;
+    const int2 info = reinterpret_cast<const int2 *>(a.info)[unit_of<RT>(a, row, first, r / RT, head / a.group)];
+    const int place = info.x, parts = info.y;
+    if (parts <= 1) return;                          // written already
+    // (starts that do not ascend may leave a unit without an owner)
+    if (place < 0 || parts > a.shares || (place & ~1) + 2 * (parts - 1) >= 2 * a.shares) return;
+    // the first part, then the first unit of each following share
+    const float *first_part = a.parts + ((int64_t)place * RT + r % RT) * (D + 4);
+    const float *others = a.parts + ((int64_t)(place & ~1) * RT + r % RT) * (D + 4);
+    auto part_of = [&](int c) { return c ? others + (int64_t)c * 2 * RT * (D + 4) : first_part; };
     float m = -__builtin_inff();
-    for (int c = lane; c < parts; c += 64) m = fmaxf(m, pm[2 * c]);
+    for (int c = lane; c < parts; c += 64) m = fmaxf(m, part_of(c)[D]);
     for (int k = 32; k; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
     const float mm = m == -__builtin_inff() ? 0.f : m;
     float l = 0.f, o[N];
     for (int j = 0; j < N; ++j) o[j] = 0.f;
 #pragma unroll 4
     for (int c = W > 1 ? wave : 0; c < parts; c += W) {
-        const float e = __builtin_amdgcn_exp2f(pm[2 * c] - mm);
-        l += e * pm[2 * c + 1];
-        for (int j = 0; j < N; ++j) o[j] += e * po[(int64_t)c * D + j * 64 + lane];
+        const float *po = part_of(c);
+        const float e = __builtin_amdgcn_exp2f(po[D] - mm);
+        l += e * po[D + 1];
+        for (int j = 0; j < N; ++j) o[j] += e * po[j * 64 + lane];
     }
     if constexpr (W > 1) {
         for (int j = 0; j < N; ++j) lds[wave * (D + 1) + j * 64 + lane] = o[j];
@@ -400,59 +477,49 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
     if (a.lse && lane == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * 0.69314718056f;
 }
 
-template <int D, bool FP8, int NT, int W>
-hipError_t launch(const AttendArgs &a, hipStream_t stream) {
+template <int D, bool FP8, int NT>
+hipError_t launch(const AttendArgs &a, const AttendPlan &p, hipStream_t stream) {
     constexpr int RT = 16 * NT;
-    constexpr size_t lds = sizeof(float) * W * RT * (D + 4 + 2);
-    if (lds > 65536) {
-        static const hipError_t once = hipFuncSetAttribute(
-            reinterpret_cast<const void *>(attend_kernel<D, FP8, NT, W>),
-            hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (once != hipSuccess) return once;
-    }
-    const int64_t slots = a.set.starts ? (int64_t)a.set.total * a.group / RT + a.set.rows
-                                       : (int64_t)a.set.rows * ((a.group + RT - 1) / RT);
-    attend_kernel<D, FP8, NT, W><<<dim3((unsigned)(slots * a.chunks), (unsigned)a.layer.heads), 64 * W, lds, stream>>>(a);
+    attend_kernel<D, FP8, NT><<<(unsigned)((p.shares + 3) / 4), 256, 0, stream>>>(a);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.chunks == 1) return e;
+    if (e != hipSuccess || !p.join) return e;
     const int64_t outs = (int64_t)a.set.total * a.heads;
-    // many parts of few results: four waves each
-    if (a.chunks > 8) join_kernel<D, 4><<<(unsigned)outs, 256, 0, stream>>>(a);
-    else join_kernel<D, 1><<<(unsigned)((outs + 3) / 4), 256, 0, stream>>>(a);
+    // results of many parts: four waves each
+    if (p.shares > 8 * p.units) join_kernel<D, RT, 4><<<(unsigned)outs, 256, 0, stream>>>(a);
+    else join_kernel<D, RT, 1><<<(unsigned)((outs + 3) / 4), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
 template <int D, bool FP8>
 hipError_t pick(const AttendArgs &a, const AttendPlan &p, hipStream_t stream) {
-    if constexpr (D < 256) {   // at 256 neither fits the registers
-        if (p.waves == 8) return launch<D, FP8, 1, 8>(a, stream);
-        if (p.tile == 32) return launch<D, FP8, 2, 4>(a, stream);
+    if constexpr (D < 256) {   // at 256 two tiles do not fit the registers
+        if (p.tile == 32) return launch<D, FP8, 2>(a, p, stream);
     }
-    return launch<D, FP8, 1, 4>(a, stream);
+    return launch<D, FP8, 1>(a, p, stream);
 }
 
 }  // namespace
 
-AttendPlan attend_plan(int64_t n, int rows, int group, int kv_heads, int width, int longest, int D) {
+AttendPlan attend_plan(int64_t n, int rows, int group, int kv_heads, int width, int longest, int D, bool starts) {
     AttendPlan p;
     const int64_t tokens = (int64_t)width * kPage;
     const int64_t len = longest > 0 && longest < tokens ? longest : tokens;
-    const int pages = (int)((len + kPage - 1) / kPage);
+    const int64_t pages = len > 0 ? (len + kPage - 1) / kPage : 1;
     // query rows of one key head and table row, on average
     const int64_t mean = (n * group + rows - 1) / rows;
     p.tile = mean > 16 && D < 256 ? 32 : 16;
-    const int64_t units = ((n * group) / p.tile + rows) * kv_heads;
-    p.waves = p.tile == 16 && D < 256 && pages <= WHOLE ? 8 : 4;
-    int64_t each = pages <= WHOLE ? pages : pages * units / WANT;
-    if (each < 8) each = 8;
-    if (each > 64) each = 64;
-    p.chunk_pages = (int)each;
-    p.chunks = pages > 0 ? (int)((pages + each - 1) / each) : 1;
+    p.units = (starts ? n * group / p.tile + rows : rows * (int64_t)((group + p.tile - 1) / p.tile)) * kv_heads;
+    // as many waves as have their registers at once: 1 to 3 per SIMD
+    const int64_t waves = D == 64 && p.tile == 16 ? 3072 : D == 256 || (D == 128 && p.tile == 32) ? 1024 : 2048;
+    p.shares = (int)(p.units * pages < waves ? p.units * pages : waves);
+    p.join = pages > 1;
+    p.line = p.units * pages;
     return p;
 }
 
-size_t attend_part_bytes(const AttendPlan &p, int64_t n, int heads, int D) {
-    return p.chunks > 1 ? sizeof(float) * (size_t)n * heads * p.chunks * (D + 2) : 0;
+size_t attend_info_bytes(const AttendPlan &p) { return ((size_t)p.units * 8 + 255) / 256 * 256; }
+size_t attend_bytes(const AttendPlan &p, int D) {
+    return attend_info_bytes(p) + (p.join ? sizeof(float) * 2 * (size_t)p.shares * p.tile * (D + 4) : 0);
 }
 
 hipError_t kv_attend(const AttendArgs &a, const AttendPlan &p, int D, int type, hipStream_t stream) {
