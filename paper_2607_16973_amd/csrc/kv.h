@@ -52,10 +52,9 @@ struct AttendArgs {
     int limit;                    // tokens of a row that are looked at
 };
 // How a call is split: query rows of a tile, tiles (units), waves that share
-// the units' pages.  line: a bound on the pages of all units.
+// the units' pages (0: a workgroup per unit).  line: a bound on the pages of all units.
 struct AttendPlan {
     int tile, shares;
-    bool join;
     int64_t units, line;
 };
 AttendPlan attend_plan(int64_t n, int rows, int group, int kv_heads, int width, int longest, int D, bool starts);

@@ -195,9 +195,10 @@ tq_status tq_kv_attend(const tq_kv_cache *cache, int32_t layer, const tq_rows *q
         if (!out || (reinterpret_cast<uintptr_t>(out) & 7)) return fail(TQ_EINVAL, "out is NULL or not 8-byte aligned");
         const int group = heads / cache->kv_heads;
         const AttendPlan p = attend_plan(n, rows, group, cache->kv_heads, width, longest, cache->head_dim, starts != nullptr);
-        if (!ws || ws_bytes < attend_bytes(p, cache->head_dim) || !aligned16(ws))
+        const size_t need = attend_bytes(p, cache->head_dim);
+        if (need && (!ws || ws_bytes < need || !aligned16(ws)))
             return fail(TQ_EINVAL, "workspace too small or not aligned");
-        if (p.line > kMost || n * heads >= kMostGroups || n * group > kMost)
+        if (p.line > kMost || p.units >= kMostGroups / 2 || n * heads >= kMostGroups || n * group > kMost)
             return fail(TQ_EUNSUPPORTED, "too many queries or tokens for one call");
         if ((st = device_ready()) != TQ_OK) return st;
         AttendArgs a;

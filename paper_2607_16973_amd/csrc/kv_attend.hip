@@ -37,6 +37,22 @@ __device__ inline float max3(float a, float b, float c) {
     return r;
 }
 
+// Rows of up to kShort pages in calls of up to kFew units have a workgroup per
+// unit: 16.6 us against 20.6 for one row of 777 tokens, 37.7 against 37.4 for
+// 64 rows of 500 to 1,500 (512 units); with 2,048 units the even shares are ahead (88 us against 70),
+// and so are they from 46 pages on (25.6 against 20.4 for one row of 2,900).
+constexpr int kShort = 24, kFew = 512;
+#ifndef CHUNK64
+#define CHUNK64 768
+#endif
+#ifndef LB64
+#define LB64 3
+#endif
+#ifndef MANY
+#define MANY 48
+#endif
+constexpr int kMany = MANY;
+
 // 16 codes -> 2 x 8 float16.
 template <bool FP8>
 __device__ inline void to_half(const uint4 &c, f16x8 *lo, f16x8 *hi) {
@@ -106,9 +122,270 @@ __device__ inline int load_queries(const AttendArgs &a, bool in, int64_t at, int
     return e;
 }
 
-// Rows of few queries (decoding, drafted tokens).  A unit is a tile of 16 NT
-// query rows of one key head of one table row, and has that row's pages to
-// go through.  All units' pages form one line, which is cut into equal
+// The codes of a page in a wave's registers, and the scales of the lane's block.
+template <int D>
+struct Page {
+    uint4 k[4][D / 64], v[D / 16];
+    float ks, vs;
+    bool fits;                       // it is in the pool and holds a token
+
+    // tile: (page, key head); the lane reads rows and coordinates of its own
+    __device__ void load_keys(const AttendArgs &a, int64_t tile, int n, int g) {
+        const char *p = a.layer.k + tile * (kPage * D) + (16 * (n >> 2) + (n & 3)) * D + g * 16;
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int u = 0; u < D / 64; ++u) k[s][u] = *reinterpret_cast<const uint4 *>(p + 4 * s * D + u * 64);
+        ks = a.layer.ks[tile * 4 + g];
+    }
+    __device__ void load_values(const AttendArgs &a, int64_t tile, int n, int g) {
+        const char *p = a.layer.v + tile * (kPage * D) + (g * D + n) * 16;
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) v[d] = *reinterpret_cast<const uint4 *>(p + d * 256);
+        vs = a.layer.vs[tile * 4 + g];
+    }
+};
+
+// NT tiles of 16 query rows of one key head: operands, positions, and what
+// the softmax has so far.
+template <int D, int NT>
+struct Rows {
+    f16x8 q[NT][D / 32];
+    float factor[NT];                // score units of a product with unscaled codes
+    int pos[NT];                     // the last key a row sees
+    int low;                         // the last one that every row sees
+    float m[NT], mv[NT], l[NT];      // maxima (log2 units) of scores and of scores with value scales; sum
+    f32x4 o[NT][D / 16];             // in units of 2^(mv - kUnit)
+
+    __device__ void begin() {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            m[i] = mv[i] = -__builtin_inff();
+            l[i] = 0.f;
+            for (int d = 0; d < D / 16; ++d) o[i][d] = {0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    // rows r0 + 16 i + n of count * group, the row's new tokens from `first` on
+    __device__ void load(const AttendArgs &a, int r0, int last, int first, int kvh, int n, int g) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const int r = min(r0 + 16 * i + n, last);
+            const int e = load_queries<D>(a, r0 + 16 * i + n <= last,
+                                          (int64_t)(first + r / a.group) * a.qt + (int64_t)(kvh * a.group + r % a.group) * a.qh, g, q[i]);
+            factor[i] = ldexpf(fabsf(a.scale2), -e);
+        }
+    }
+    // true_len - count: the position of the row's first new token
+    __device__ void place(const AttendArgs &a, int r0, int last, int origin, int len, int n) {
+        low = min(origin + r0 / a.group, len - 1);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) pos[i] = min(origin + min(r0 + 16 * i + n, last) / a.group, len - 1);
+    }
+};
+
+// One page: number `index` of a row of len tokens.  next_keys() and
+// next_values() are called when the page's own are no longer needed.
+template <int D, bool FP8, int NT, class K, class V>
+__device__ inline void page_step(Rows<D, NT> &t, Page<D> &page, int index, int len, int g, K next_keys, V next_values) {
+    constexpr int DT = D / 16;
+    // S^T of the page
+    f32x4 s[NT][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        for (int i = 0; i < NT; ++i) s[i][j] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < D / 64; ++u) {
+            f16x8 lo, hi;
+            to_half<FP8>(page.k[j][u], &lo, &hi);
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                s[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, t.q[i][2 * u], s[i][j], 0, 0, 0);
+                s[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, t.q[i][2 * u + 1], s[i][j], 0, 0, 0);
+            }
+        }
+    }
+    const bool here = page.fits;
+    const float kscale = page.ks;
+    next_keys();
+    __builtin_amdgcn_sched_barrier(0);
+    const int base = index * kPage + 16 * g;         // position of the lane's first token
+    float vlog = page.vs > 0.f ? __log2f(page.vs) : -__builtin_inff();
+    // A page that holds the row's end may hold anything past it: those
+    // codes and scales are taken out before they meet a zero weight.
+    if ((index + 1) * kPage > len || !here) {
+        const int left = here ? min(max(len - base, 0), 16) : 0;
+        if (left == 0) vlog = -__builtin_inff();
+#pragma unroll
+        for (int d = 0; d < DT; ++d) page.v[d] = keep_tokens(page.v[d], left);
+    }
+    const bool masked = (index + 1) * kPage - 1 > t.low || !here;
+
+    f16x8 w[NT][2], wl[NT][2];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        // never 0, so that a masked score stays -inf (a NaN scale of an unused block goes too)
+        const float f = fmaxf(t.factor[i] * kscale, 0x1p-126f);
+        if (masked) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (base + j > t.pos[i] || !here) s[i][j >> 2][j & 3] = -__builtin_inff();
+        }
+        float big = max3(s[i][0][0], s[i][0][1], s[i][0][2]);
+#pragma unroll
+        for (int j = 3; j < 15; j += 2) big = max3(big, s[i][j >> 2][j & 3], s[i][(j + 1) >> 2][(j + 1) & 3]);
+        big = fmaxf(big, s[i][3][3]) * f;
+        const float top1 = max_of_groups(big), top2 = max_of_groups(big + vlog);
+        if (__any(top1 > t.m[i] + kLag || top2 > t.mv[i] + kLag)) {
+            const float m1 = fmaxf(t.m[i], top1), m2 = fmaxf(t.mv[i], top2);
+            t.l[i] *= t.m[i] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(t.m[i] - m1);
+            const float back = t.mv[i] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(t.mv[i] - m2);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) t.o[i][d] *= back;
+            t.m[i] = m1;
+            t.mv[i] = m2;
+        }
+        const float m1 = t.m[i] == -__builtin_inff() ? 0.f : t.m[i], m2 = t.mv[i] == -__builtin_inff() ? 0.f : t.mv[i];
+        const float gain = __builtin_amdgcn_exp2f(fminf(vlog + (m1 - m2) + kUnit, 126.f));
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const float e = __builtin_amdgcn_exp2f(scaled_less(s[i][j >> 2][j & 3], f, m1));
+            sum += e;
+            const float y = e * gain;
+            const _Float16 hi = (_Float16)y;
+            w[i][j >> 3][j & 7] = hi;
+            wl[i][j >> 3][j & 7] = (_Float16)(y - (float)hi);
+        }
+        t.l[i] += sum;
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+        f16x8 lo, hi;
+        to_half<FP8>(page.v[d], &lo, &hi);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            t.o[i][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, w[i][0], t.o[i][d], 0, 0, 0);
+            t.o[i][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, w[i][1], t.o[i][d], 0, 0, 0);
+            t.o[i][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, wl[i][0], t.o[i][d], 0, 0, 0);
+            t.o[i][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, wl[i][1], t.o[i][d], 0, 0, 0);
+        }
+    }
+    next_values();
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// The tile (page, key head) of a page id; page.fits says whether to use it
+// (any: the page holds a token of the row).
+template <int D>
+__device__ inline int64_t take(const AttendArgs &a, Page<D> &page, int id, bool any, int kvh) {
+    const bool in = id >= 0 && id < a.layer.pages;
+    page.fits = in && any;
+    if (!in && any && a.layer.status && __lane_id() == 0) atomicOr(a.layer.status, TQ_KV_BAD_PAGE);
+    return (int64_t)(page.fits ? id : 0) * a.layer.heads + kvh;
+}
+
+__device__ inline void write4(const AttendArgs &a, int64_t at, f32x4 o) {
+    unsigned short h[4];
+    for (int k = 0; k < 4; ++k) h[k] = float_bits16(o[k], a.bf16);
+    uint2 u;
+    __builtin_memcpy(&u, h, 8);
+    *reinterpret_cast<uint2 *>(static_cast<unsigned short *>(a.out) + at) = u;
+}
+__device__ inline float log_sum(float m, float l) {
+    return l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * 0.69314718056f;
+}
+__device__ inline float inverse(float l) { return l > 0.f || l != l ? 1.f / l : 0.f; }
+
+// Short rows: a workgroup has a unit -- a tile of 16 NT query rows of one key
+// head of one table row -- to itself, its W waves take every W-th page and
+// are joined through LDS: one launch, where what a call costs is latency.
+template <int D, bool FP8, int NT, int W>
+__global__ __launch_bounds__(64 * W) void attend_short_kernel(AttendArgs a) {
+    constexpr int DT = D / 16, RT = 16 * NT;
+    extern __shared__ __align__(16) float lds[];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int kvh = blockIdx.x % a.layer.heads;
+    int64_t slot = blockIdx.x / a.layer.heads;
+    int row, first, count;
+    if (a.set.starts) {
+        row = slot_row(a.set.starts, a.set.rows, slot, a.group, RT, 1);
+        slot -= slot_begin(a.set.starts, row, a.group, RT, 1);
+    } else {   // one token per row: its group in ceil(group / RT) tiles
+        const int per = (a.group + RT - 1) / RT;
+        row = (int)(slot / per);
+        slot %= per;
+    }
+    row_tokens(a.set.starts, row, a.set.total, &first, &count);
+    const int rows = count * a.group;
+    if (slot < 0 || slot * RT >= rows) return;       // the whole workgroup
+    const int r0 = (int)slot * RT, last = min(rows - 1, r0 + RT - 1);
+
+    // the row's length, the wave's first page id and the queries at once
+    const int *table = a.set.tables + (int64_t)row * a.set.width;
+    const int true_len = a.set.lens[row];
+    int ahead = wave < a.set.width ? table[wave] : -1;
+    Rows<D, NT> t;
+    t.load(a, r0, last, first, kvh, n, g);
+    const int len = min(true_len, a.limit);
+    t.place(a, r0, last, true_len - count, len, n);
+    t.begin();
+    const int top = min(true_len - count + last / a.group, len - 1);
+    const int end = top < 0 ? 0 : top / kPage + 1;
+    Page<D> page;
+    if (wave < end) {
+        const int64_t tile = take(a, page, __builtin_amdgcn_readfirstlane(ahead), true, kvh);
+        page.load_keys(a, tile, n, g);
+        page.load_values(a, tile, n, g);
+        if (wave + W < end) ahead = table[wave + W];
+    }
+    for (int p = wave; p < end; p += W) {
+        int64_t tile = 0;
+        page_step<D, FP8, NT>(t, page, p, len, g, [&] {
+            if (p + W >= end) return;
+            tile = take(a, page, __builtin_amdgcn_readfirstlane(ahead), true, kvh);
+            page.load_keys(a, tile, n, g);
+            if (p + 2 * W < end) ahead = table[p + 2 * W];
+        }, [&] {
+            if (p + W < end) page.load_values(a, tile, n, g);
+        });
+    }
+
+    constexpr int OS = D + 4;                        // LDS row, off the banks' period
+    float *lm = lds + W * RT * OS;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        const float sum = sum_of_groups(t.l[i]);
+        // to units of 2^m, which the waves have in common with the sum
+        const float back = t.mv[i] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(t.mv[i] - t.m[i] - kUnit);
+        for (int d = 0; d < DT; ++d)
+            *reinterpret_cast<f32x4 *>(lds + ((wave * RT + 16 * i + n) * OS + d * 16 + g * 4)) = t.o[i][d] * back;
+        if (g == 0) {
+            lm[(wave * RT + 16 * i + n) * 2] = t.m[i];
+            lm[(wave * RT + 16 * i + n) * 2 + 1] = sum;
+        }
+    }
+    __syncthreads();
+    // four coordinates of a row per thread
+    for (int j = threadIdx.x; j < RT * (D / 4); j += 64 * W) {
+        const int tr = j / (D / 4), d = (j % (D / 4)) * 4, r = r0 + tr;
+        if (r > last) continue;
+        float mt = -__builtin_inff();
+        for (int w = 0; w < W; ++w) mt = fmaxf(mt, lm[(w * RT + tr) * 2]);
+        const float mm = mt == -__builtin_inff() ? 0.f : mt;
+        float sum = 0.f;
+        f32x4 ot = {0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < W; ++w) {
+            const float e = __builtin_amdgcn_exp2f(lm[(w * RT + tr) * 2] - mm);
+            sum += e * lm[(w * RT + tr) * 2 + 1];
+            ot += e * *reinterpret_cast<const f32x4 *>(lds + ((w * RT + tr) * OS + d));
+        }
+        const int64_t at = (int64_t)(first + r / a.group) * a.heads + kvh * a.group + r % a.group;
+        write4(a, at * D + d, ot * inverse(sum));
+        if (a.lse && d == 0) a.lse[at] = log_sum(mt, sum);
+    }
+}
+
+// Longer rows.  All units' pages form one line, which is cut into equal
 // shares, one per wave of the grid: rows of very different lengths load the
 // machine evenly, and a wave has the next page's codes on the way while it
 // works, across units too.  A unit that lies in one share is written out at
@@ -165,16 +442,11 @@ __device__ inline int64_t unit_of(const AttendArgs &a, int row, int first, int t
     return (slot + tile) * a.layer.heads + kvh;
 }
 
-template <int D, bool FP8, int NT>
-__global__ __launch_bounds__(256) void attend_kernel(AttendArgs a) {
-    constexpr int KS = D / 32;                       // 32-wide steps of the first product
-    constexpr int DT = D / 16;
-    constexpr int RT = 16 * NT;
-    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    const int share = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-    const int heads = a.layer.heads;
-
-    // the line's length, the wave's share [x, end) and where x lies
+// The pages [x, end) of the line that a share has (each: the shares' size), and
+// where x lies; false if there are none.  Called by whole waves.
+template <int RT>
+__device__ inline bool find_share(const AttendArgs &a, int share, int *each, int *x, int *end, Place *cur) {
+    const int lane = __lane_id(), heads = a.layer.heads;
     auto pages_at = [&](int row) {
         Place p;
         if (row >= a.set.rows) return 0;
@@ -193,229 +465,375 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendArgs a) {
         sums = running(pages_at(base + lane));
         total += __builtin_amdgcn_readlane(sums, 63);
     }
-    const int each = (total + a.shares - 1) / a.shares;
-    const int x = share * each, end = min(x + each, total);
-    if (x >= end) return;
-    Place cur;
-    {
-        int before = 0;
-        for (int base = 0;; base += 64) {
-            if (a.set.rows > 64) sums = running(pages_at(base + lane));
-            const uint64_t past = __ballot(before + sums > x);
-            if (past) {
-                const int at = __builtin_ctzll(past);
-                if (at) before += __builtin_amdgcn_readlane(sums, at - 1);
-                to_row<RT>(a, base + at, &cur);
-                break;
-            }
-            before += __builtin_amdgcn_readlane(sums, 63);
+    *each = (total + a.shares - 1) / a.shares;
+    *x = share * *each;
+    *end = min(*x + *each, total);
+    if (*x >= *end) return false;
+    int before = 0;
+    for (int base = 0;; base += 64) {
+        if (a.set.rows > 64) sums = running(pages_at(base + lane));
+        const uint64_t past = __ballot(before + sums > *x);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            if (at) before += __builtin_amdgcn_readlane(sums, at - 1);
+            to_row<RT>(a, base + at, cur);
+            break;
         }
-        const int within = x - before, unit = within / cur.pages;
-        cur.page = within % cur.pages;
-        cur.tile = unit / heads;
-        cur.kvh = unit % heads;
+        before += __builtin_amdgcn_readlane(sums, 63);
     }
+    const int within = *x - before, unit = within / cur->pages;
+    cur->page = within % cur->pages;
+    cur->tile = unit / heads;
+    cur->kvh = unit % heads;
+    return true;
+}
 
-    // what a page needs: its codes and the scales of the lane's block
-    uint4 kc[4][D / 64], vc[DT];
-    const int krow = (16 * (n >> 2) + (n & 3)) * D + g * 16, vrow = (g * D + n) * 16;
-    auto any_in = [&](const Place &p) { return p.page * kPage < min(p.len, a.limit); };
-    auto id_of = [&](const Place &p) { return any_in(p) ? a.set.tables[(int64_t)p.row * a.set.width + p.page] : -1; };
-    bool fits = false;
-    auto tile_of = [&](const Place &p, int page) {
-        const bool in = page >= 0 && page < a.layer.pages, any = any_in(p);
-        fits = in && any;
-        if (!in && any && a.layer.status && lane == 0) atomicOr(a.layer.status, TQ_KV_BAD_PAGE);
-        return (int64_t)(fits ? page : 0) * heads + p.kvh;
-    };
-    auto load_keys = [&](int64_t tile) {
-        const char *kp = a.layer.k + tile * (kPage * D) + krow;
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-            for (int u = 0; u < D / 64; ++u) kc[s][u] = *reinterpret_cast<const uint4 *>(kp + 4 * s * D + u * 64);
-    };
-    auto load_values = [&](int64_t tile) {
-        const char *vp = a.layer.v + tile * (kPage * D) + vrow;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) vc[d] = *reinterpret_cast<const uint4 *>(vp + d * 256);
-    };
-    int64_t tile = tile_of(cur, __builtin_amdgcn_readfirstlane(id_of(cur)));
-    load_keys(tile);
-    float ks = a.layer.ks[tile * 4 + g], vs = a.layer.vs[tile * 4 + g];
-    load_values(tile);
+__device__ inline bool any_in(const AttendArgs &a, const Place &p) { return p.page * kPage < min(p.len, a.limit); }
+__device__ inline int id_of(const AttendArgs &a, const Place &p) {
+    return any_in(a, p) ? a.set.tables[(int64_t)p.row * a.set.width + p.page] : -1;
+}
+// Who begins a unit says where its parts are: at: the line's position of the page `cur`.
+template <int RT>
+__device__ inline void tell_parts(const AttendArgs &a, const Place &cur, int at, int each, int place) {
+    const int begin = at - cur.page, finish = begin + cur.pages - 1;
+    reinterpret_cast<int2 *>(a.info)[unit_of<RT>(a, cur.row, cur.first, cur.tile, cur.kvh)] =
+        make_int2(place, finish / each - begin / each + 1);
+}
+
+template <int D, bool FP8, int NT>
+__global__ __launch_bounds__(256) void attend_kernel(AttendArgs a) {
+    constexpr int DT = D / 16, RT = 16 * NT;
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int share = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    int each, x, end;
+    Place cur;
+    if (!find_share<RT>(a, share, &each, &x, &end, &cur)) return;
+
+    Page<D> page;
+    int64_t tile = take(a, page, __builtin_amdgcn_readfirstlane(id_of(a, cur)), any_in(a, cur), cur.kvh);
+    page.load_keys(a, tile, n, g);
+    page.load_values(a, tile, n, g);
     Place next = cur;                                // the page whose codes come next, its id on the way
     int ahead = 0;
     if (x + 1 < end) {
         advance<RT>(a, &next);
-        ahead = id_of(next);
+        ahead = id_of(a, next);
     }
 
-    f16x8 q[NT][KS];
-    float factor[NT];
-    int pos[NT];                                     // the last key a row sees
-    int top = -1, low = -1;                          // the last one any row and every row sees
-    float m[NT], mv[NT], l[NT];                      // maxima (log2 units) of scores and of scores with value scales; sum
-    f32x4 o[NT][DT];                                 // in units of 2^(mv - kUnit)
+    Rows<D, NT> t;
     int from = cur.page;                             // the first page of the unit in this share
     bool open = true;                                // a unit begins
 
     for (int at = x; at < end; ++at) {
         const int len = min(cur.len, a.limit);
-        const int rows = cur.count * a.group, r0 = cur.tile * RT, last = min(rows - 1, r0 + RT - 1);
+        const int r0 = cur.tile * RT, last = min(cur.count * a.group - 1, r0 + RT - 1);
         if (open) {
             from = cur.page;
-            top = min(cur.len - cur.count + last / a.group, len - 1);
-            low = min(cur.len - cur.count + r0 / a.group, len - 1);
-#pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                const int r = min(r0 + 16 * i + n, last), token = r / a.group;
-                pos[i] = min(cur.len - cur.count + token, len - 1);
-                const int e = load_queries<D>(a, r0 + 16 * i + n <= last,
-                                              (int64_t)(cur.first + token) * a.qt + (int64_t)(cur.kvh * a.group + r % a.group) * a.qh, g, q[i]);
-                factor[i] = ldexpf(fabsf(a.scale2), -e);
-                m[i] = mv[i] = -__builtin_inff();
-                l[i] = 0.f;
-                for (int d = 0; d < DT; ++d) o[i][d] = {0.f, 0.f, 0.f, 0.f};
-            }
+            t.load(a, r0, last, cur.first, cur.kvh, n, g);
+            t.place(a, r0, last, cur.len - cur.count, len, n);
+            t.begin();
             open = false;
         }
-        // S^T of the page
-        f32x4 s[NT][4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            for (int i = 0; i < NT; ++i) s[i][j] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int u = 0; u < D / 64; ++u) {
-                f16x8 lo, hi;
-                to_half<FP8>(kc[j][u], &lo, &hi);
-#pragma unroll
-                for (int i = 0; i < NT; ++i) {
-                    s[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, q[i][2 * u], s[i][j], 0, 0, 0);
-                    s[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, q[i][2 * u + 1], s[i][j], 0, 0, 0);
-                }
-            }
-        }
-        const bool here = fits, more = at + 1 < end;
-        const float kscale = ks;
-        const Place then = next;                     // the next page's keys
-        if (more) {
-            tile = tile_of(next, __builtin_amdgcn_readfirstlane(ahead));
-            load_keys(tile);
-            ks = a.layer.ks[tile * 4 + g];
+        const bool more = at + 1 < end;
+        const Place then = next;
+        page_step<D, FP8, NT>(t, page, cur.page, len, g, [&] {
+            if (!more) return;
+            tile = take(a, page, __builtin_amdgcn_readfirstlane(ahead), any_in(a, next), next.kvh);
+            page.load_keys(a, tile, n, g);
             if (at + 2 < end) {
                 advance<RT>(a, &next);
-                ahead = id_of(next);
+                ahead = id_of(a, next);
             }
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        const int base = cur.page * kPage + 16 * g;  // position of the lane's first token
-        float vlog = vs > 0.f ? __log2f(vs) : -__builtin_inff();
-        // A page that holds the row's end may hold anything past it: those
-        // codes and scales are taken out before they meet a zero weight.
-        if ((cur.page + 1) * kPage > len || !here) {
-            const int left = here ? min(max(len - base, 0), 16) : 0;
-            if (left == 0) vlog = -__builtin_inff();
-#pragma unroll
-            for (int d = 0; d < DT; ++d) vc[d] = keep_tokens(vc[d], left);
-        }
-        const bool masked = (cur.page + 1) * kPage - 1 > low || !here;
-
-        f16x8 w[NT][2], wl[NT][2];
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            // never 0, so that a masked score stays -inf (a NaN scale of an unused block goes too)
-            const float f = fmaxf(factor[i] * kscale, 0x1p-126f);
-            if (masked) {
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (base + j > pos[i] || !here) s[i][j >> 2][j & 3] = -__builtin_inff();
-            }
-            float big = max3(s[i][0][0], s[i][0][1], s[i][0][2]);
-#pragma unroll
-            for (int j = 3; j < 15; j += 2) big = max3(big, s[i][j >> 2][j & 3], s[i][(j + 1) >> 2][(j + 1) & 3]);
-            big = fmaxf(big, s[i][3][3]) * f;
-            const float top1 = max_of_groups(big), top2 = max_of_groups(big + vlog);
-            if (__any(top1 > m[i] + kLag || top2 > mv[i] + kLag)) {
-                const float m1 = fmaxf(m[i], top1), m2 = fmaxf(mv[i], top2);
-                l[i] *= m[i] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m[i] - m1);
-                const float back = mv[i] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(mv[i] - m2);
-#pragma unroll
-                for (int d = 0; d < DT; ++d) o[i][d] *= back;
-                m[i] = m1;
-                mv[i] = m2;
-            }
-            const float m1 = m[i] == -__builtin_inff() ? 0.f : m[i], m2 = mv[i] == -__builtin_inff() ? 0.f : mv[i];
-            const float gain = __builtin_amdgcn_exp2f(fminf(vlog + (m1 - m2) + kUnit, 126.f));
-            float sum = 0.f;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const float e = __builtin_amdgcn_exp2f(scaled_less(s[i][j >> 2][j & 3], f, m1));
-                sum += e;
-                const float y = e * gain;
-                const _Float16 hi = (_Float16)y;
-                w[i][j >> 3][j & 7] = hi;
-                wl[i][j >> 3][j & 7] = (_Float16)(y - (float)hi);
-            }
-            l[i] += sum;
-        }
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-            f16x8 lo, hi;
-            to_half<FP8>(vc[d], &lo, &hi);
-#pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                o[i][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, w[i][0], o[i][d], 0, 0, 0);
-                o[i][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, w[i][1], o[i][d], 0, 0, 0);
-                o[i][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, wl[i][0], o[i][d], 0, 0, 0);
-                o[i][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, wl[i][1], o[i][d], 0, 0, 0);
-            }
-        }
-        if (more) {                                  // and its values
-            load_values(tile);
-            vs = a.layer.vs[tile * 4 + g];
-        }
-        __builtin_amdgcn_sched_barrier(0);
+        }, [&] {
+            if (more) page.load_values(a, tile, n, g);
+        });
 
         if (cur.page + 1 == cur.pages || !more) {    // the unit, or the share, ends here
             const bool whole = from == 0 && cur.page + 1 == cur.pages;
             const int place = 2 * share + (at - x == cur.page - from ? 0 : 1);   // the share's first unit, or its last
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
-                const float sum = sum_of_groups(l[i]);
+                const float sum = sum_of_groups(t.l[i]);
                 // to units of 2^m, which the parts have in common with the sum
-                const float back = mv[i] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(mv[i] - m[i] - kUnit);
+                const float back = t.mv[i] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(t.mv[i] - t.m[i] - kUnit);
                 const int r = r0 + 16 * i + n;
                 if (r <= last) {
                     if (whole) {
                         const int64_t to = (int64_t)(cur.first + r / a.group) * a.heads + cur.kvh * a.group + r % a.group;
-                        const float inv = sum > 0.f || sum != sum ? back / sum : 0.f;
+                        const float inv = back * inverse(sum);
 #pragma unroll
-                        for (int d = 0; d < DT; ++d) {
-                            unsigned short h[4];
-                            for (int k = 0; k < 4; ++k) h[k] = float_bits16(o[i][d][k] * inv, a.bf16);
-                            uint2 u;
-                            __builtin_memcpy(&u, h, 8);
-                            *reinterpret_cast<uint2 *>(static_cast<unsigned short *>(a.out) + to * D + d * 16 + g * 4) = u;
-                        }
-                        if (a.lse && g == 0) a.lse[to] = sum == 0.f ? -__builtin_inff() : (m[i] + __log2f(sum)) * 0.69314718056f;
+                        for (int d = 0; d < DT; ++d) write4(a, to * D + d * 16 + g * 4, t.o[i][d] * inv);
+                        if (a.lse && g == 0) a.lse[to] = log_sum(t.m[i], sum);
                     } else {
                         float *po = a.parts + ((int64_t)place * RT + 16 * i + n) * (D + 4);
 #pragma unroll
-                        for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4 *>(po + d * 16 + g * 4) = o[i][d] * back;
+                        for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4 *>(po + d * 16 + g * 4) = t.o[i][d] * back;
                         if (g == 0) {
-                            po[D] = m[i];
+                            po[D] = t.m[i];
                             po[D + 1] = sum;
                         }
                     }
                 }
             }
-            // who begins a unit says where its parts are
-            if (from == 0 && lane == 0) {
-                const int begin = at - cur.page, finish = begin + cur.pages - 1;   // in the line
-                reinterpret_cast<int2 *>(a.info)[unit_of<RT>(a, cur.row, cur.first, cur.tile, cur.kvh)] =
-                    make_int2(place, finish / each - begin / each + 1);
+            if (from == 0 && lane == 0) tell_parts<RT>(a, cur, at, each, place);
+            open = true;
+        }
+        cur = then;
+    }
+}
+
+// Many queries per row (a chunk of a prompt against what is cached): 32 query rows per
+// wave and 128 per workgroup, one share of the line per workgroup.  A page's
+// codes become float16 once per workgroup, on their way through LDS, and
+// the products are 32x32x16; the codes of the page after next are on their
+// way in registers meanwhile.  A lane's 32 scores of a page are 8 of each of its
+// four blocks, so scales are uniform values again.  Bound by the
+// exponentials at d = 64, by the matrix cores beyond.  PARTS: the weights go
+// to the product in that many float16 parts (two for float16 results, whose
+// own rounding is as small as that of the weights).
+template <int D, bool FP8, int PARTS>
+__global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? LB64 : 2) void attend_chunk_kernel(AttendArgs a) {
+    constexpr int KS = D / 16, DT = D / 32, CH = D / 8, RT = 128, RAW = D / 64;
+    constexpr int TILE = kPage * D * 2;              // bytes of a page's keys in float16
+    extern __shared__ __align__(16) char store[];    // [2][keys [64][D], values [D][64]]
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+    const int share = blockIdx.x;
+    int each, x, end;
+    Place cur;
+    if (!find_share<RT>(a, share, &each, &x, &end, &cur)) return;
+
+    // codes of a page on their way, with what to do with them
+    uint4 kraw[RAW], vraw[RAW];
+    struct Coming {
+        float ks[4], vs[4];
+        bool fits;
+    } coming, here;
+    auto load = [&](const Place &p, int id) {
+        const bool in = id >= 0 && id < a.layer.pages, any = any_in(a, p);
+        coming.fits = in && any;
+        if (!in && any && a.layer.status && threadIdx.x == 0) atomicOr(a.layer.status, TQ_KV_BAD_PAGE);
+        const int64_t tile = (int64_t)(coming.fits ? id : 0) * a.layer.heads + p.kvh;
+        const uint4 *kp = reinterpret_cast<const uint4 *>(a.layer.k + tile * (kPage * D)) + threadIdx.x;
+        const uint4 *vp = reinterpret_cast<const uint4 *>(a.layer.v + tile * (kPage * D)) + threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < RAW; ++i) {
+            kraw[i] = kp[i * 256];
+            vraw[i] = vp[i * 256];
+        }
+        for (int b = 0; b < 4; ++b) {
+            coming.ks[b] = a.layer.ks[tile * 4 + b];
+            coming.vs[b] = a.layer.vs[tile * 4 + b];
+        }
+        // a page that holds the row's end may hold anything past it
+        const int len = min(p.len, a.limit);
+        if ((p.page + 1) * kPage > len || !coming.fits) {
+#pragma unroll
+            for (int i = 0; i < RAW; ++i) {
+                const int b = (threadIdx.x + i * 256) / D, base = p.page * kPage + b * kBlock;
+                vraw[i] = keep_tokens(vraw[i], coming.fits ? min(max(len - base, 0), kBlock) : 0);
             }
+            for (int b = 0; b < 4; ++b)
+                if (!coming.fits || p.page * kPage + b * kBlock >= len) coming.vs[b] = 0.f;
+        }
+    };
+    auto put = [&](int half) {
+        char *base = store + half * 2 * TILE;
+#pragma unroll
+        for (int i = 0; i < RAW; ++i) {
+            const int c = threadIdx.x + i * 256;
+            f16x8 lo, hi;
+            to_half<FP8>(kraw[i], &lo, &hi);
+            const int kr = c / (D / 16), p = 2 * (c % (D / 16)), swap = kr & (CH - 1) & 15;
+            *reinterpret_cast<f16x8 *>(base + (kr * CH + (p ^ swap)) * 16) = lo;
+            *reinterpret_cast<f16x8 *>(base + (kr * CH + ((p + 1) ^ swap)) * 16) = hi;
+            to_half<FP8>(vraw[i], &lo, &hi);
+            // the order in which the scores come out: tokens 0-3, 8-11 for lanes
+            // below 32, 4-7, 12-15 for the others
+            const int b = c / D, d = c % D, vswap = (d >> 1) & 7;
+            const uint4 l = __builtin_bit_cast(uint4, lo), u = __builtin_bit_cast(uint4, hi);
+            *reinterpret_cast<uint4 *>(base + TILE + (d * 8 + ((2 * b) ^ vswap)) * 16) = make_uint4(l.x, l.y, u.x, u.y);
+            *reinterpret_cast<uint4 *>(base + TILE + (d * 8 + ((2 * b + 1) ^ vswap)) * 16) = make_uint4(l.z, l.w, u.z, u.w);
+        }
+    };
+
+    load(cur, __builtin_amdgcn_readfirstlane(id_of(a, cur)));
+    Place next = cur;                                // the page that is in kraw, vraw
+    int ahead = -1;
+    Place after = cur;                               // the one whose id is on its way
+    put(0);
+    here = coming;
+    if (x + 1 < end) {
+        advance<RT>(a, &next);
+        load(next, __builtin_amdgcn_readfirstlane(id_of(a, next)));
+        after = next;
+        if (x + 2 < end) {
+            advance<RT>(a, &after);
+            ahead = id_of(a, after);
+        }
+    }
+
+    f16x8 q[KS];
+    float factor = 0.f, m = 0.f, mv = 0.f, l = 0.f;
+    f32x16 o[DT];
+    int pos = -1, from = cur.page, low = -1, top = -1;
+    bool open = true, wild = false;
+    for (int at = x; at < end; ++at) {
+        const int len = min(cur.len, a.limit);
+        const int r0 = cur.tile * RT, last = min(cur.count * a.group - 1, r0 + RT - 1), origin = cur.len - cur.count;
+        if (open) {
+            from = cur.page;
+            low = min(origin + r0 / a.group, len - 1);
+            top = min(origin + last / a.group, len - 1);
+            const int r = r0 + wave * 32 + n, rr = min(r, last);
+            pos = min(origin + rr / a.group, len - 1);
+            float y[KS][8], big = 0.f;
+            const int64_t qat = (int64_t)(cur.first + rr / a.group) * a.qt + (int64_t)(cur.kvh * a.group + rr % a.group) * a.qh + h * 8;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                load8(a.q, qat + s * 16, a.bf16, a.wide, y[s]);
+                for (int j = 0; j < 8; ++j) big = fmaxf(big, fabsf(y[s][j]) < __builtin_inff() ? fabsf(y[s][j]) : 0.f);
+            }
+            big = max_of_halves(big);
+            int e;
+            frexpf(big, &e);
+            e = big > 0.f ? 15 - e : 0;
+            const float sign = a.scale2 < 0.f ? -1.f : 1.f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+                for (int j = 0; j < 8; ++j) q[s][j] = (_Float16)(sign * ldexpf(y[s][j], e));
+            factor = ldexpf(fabsf(a.scale2), -e);
+            m = mv = -__builtin_inff();
+            l = 0.f;
+            wild = false;
+            for (int d = 0; d < DT; ++d)
+                for (int j = 0; j < 16; ++j) o[d][j] = 0.f;
+            open = false;
+        }
+        const char *half = store + ((at - x) & 1) * 2 * TILE;
+        __syncthreads();
+        const bool use = cur.page * kPage <= top;    // a row of the tile sees the page
+        f32x16 s[2];
+        if (use) {
+            for (int t = 0; t < 2; ++t)
+                for (int j = 0; j < 16; ++j) s[t][j] = 0.f;
+#pragma unroll
+            for (int c = 0; c < KS; ++c)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const int kr = t * 32 + n;
+                    const f16x8 k = *reinterpret_cast<const f16x8 *>(half + (kr * CH + ((2 * c + h) ^ (kr & (CH - 1) & 15))) * 16);
+                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[c], s[t], 0, 0, 0);
+                }
+        }
+        const Coming now = here;
+        const Place then = next;
+        if (at + 1 < end) {
+            put((at - x + 1) & 1);
+            here = coming;
+            if (at + 2 < end) {
+                next = after;
+                load(next, __builtin_amdgcn_readfirstlane(ahead));
+                if (at + 3 < end) {
+                    advance<RT>(a, &after);
+                    ahead = id_of(a, after);
+                }
+            }
+        }
+        if (use) {
+            if ((cur.page + 1) * kPage - 1 > low || !now.fits) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    const int key = cur.page * kPage + (j >> 4) * 32 + ((j & 15) >> 2) * 8 + 4 * h + (j & 3);
+                    if (key > pos || !now.fits) s[j >> 4][j & 15] = -__builtin_inff();
+                }
+            }
+            float f[4], vlog[4], top1 = -__builtin_inff(), top2 = -__builtin_inff();
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                f[b] = fmaxf(factor * now.ks[b], 0x1p-126f);   // never 0: a masked score stays -inf
+                vlog[b] = now.vs[b] > 0.f ? __log2f(now.vs[b]) : -__builtin_inff();
+                float big = max3(s[b >> 1][8 * (b & 1)], s[b >> 1][8 * (b & 1) + 1], s[b >> 1][8 * (b & 1) + 2]);
+                big = max3(big, s[b >> 1][8 * (b & 1) + 3], s[b >> 1][8 * (b & 1) + 4]);
+                big = max3(big, s[b >> 1][8 * (b & 1) + 5], s[b >> 1][8 * (b & 1) + 6]);
+                big = fmaxf(big, s[b >> 1][8 * (b & 1) + 7]) * f[b];
+                top1 = fmaxf(top1, big);
+                top2 = fmaxf(top2, big + vlog[b]);
+            }
+            top1 = max_of_halves(top1);
+            top2 = max_of_halves(top2);
+            if (__any(top1 > m + kLag || top2 > mv + kLag)) {
+                const float m1 = fmaxf(m, top1), m2 = fmaxf(mv, top2);
+                l *= m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - m1);
+                const float back = mv == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(mv - m2);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[d] *= back;
+                m = m1;
+                mv = m2;
+                wild = __any(fabsf(m1) > 0x1p20f && m1 > -__builtin_inff());
+            }
+            const float m1 = m == -__builtin_inff() ? 0.f : m, m2 = mv == -__builtin_inff() ? 0.f : mv;
+            float shift = -m1;
+            if (wild) {   // products and maximum rounded alike: the largest score gives 0
+#pragma unroll
+                for (int j = 0; j < 32; ++j) s[j >> 4][j & 15] = scaled_less(s[j >> 4][j & 15], f[j >> 3], m1);
+                for (int b = 0; b < 4; ++b) f[b] = 1.f;
+                shift = 0.f;
+            }
+            float sum[2] = {0.f, 0.f};
+            f16x8 w[4], wl[PARTS > 1 ? 4 : 1];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const float gain = __builtin_amdgcn_exp2f(fminf(vlog[b] + (m1 - m2) + kUnit, 126.f));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b >> 1][8 * (b & 1) + i], f[b], shift));
+                    sum[i & 1] += e;
+                    const float y = e * gain;
+                    w[b][i] = (_Float16)y;
+                    if constexpr (PARTS > 1) wl[b][i] = (_Float16)(y - (float)w[b][i]);
+                }
+            }
+            l += sum[0] + sum[1];
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    const int e = d * 32 + n;
+                    const f16x8 v = *reinterpret_cast<const f16x8 *>(half + TILE + (e * 8 + ((2 * b + h) ^ ((e >> 1) & 7))) * 16);
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, w[b], o[d], 0, 0, 0);
+                    if constexpr (PARTS > 1) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, wl[b], o[d], 0, 0, 0);
+                }
+        }
+
+        if (cur.page + 1 == cur.pages || at + 1 == end) {
+            const bool whole = from == 0 && cur.page + 1 == cur.pages;
+            const int place = 2 * share + (at - x == cur.page - from ? 0 : 1);   // the share's first unit, or its last
+            const float sum = sum_of_halves(l);
+            const float back = mv == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(mv - m - kUnit);
+            const int r = r0 + wave * 32 + n;
+            if (r <= last) {
+                const int64_t to = (int64_t)(cur.first + r / a.group) * a.heads + cur.kvh * a.group + r % a.group;
+                float *po = a.parts + ((int64_t)place * RT + wave * 32 + n) * (D + 4);
+                const float k = whole ? back * inverse(sum) : back;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const f32x4 y = {o[d][4 * j] * k, o[d][4 * j + 1] * k, o[d][4 * j + 2] * k, o[d][4 * j + 3] * k};
+                        const int e = d * 32 + 8 * j + 4 * h;
+                        if (whole) write4(a, to * D + e, y);
+                        else *reinterpret_cast<f32x4 *>(po + e) = y;
+                    }
+                if (h == 0) {
+                    if (whole) {
+                        if (a.lse) a.lse[to] = log_sum(m, sum);
+                    } else {
+                        po[D] = m;
+                        po[D + 1] = sum;
+                    }
+                }
+            }
+            if (from == 0 && threadIdx.x == 0) tell_parts<RT>(a, cur, at, each, place);
             open = true;
         }
         cur = then;
@@ -471,10 +889,10 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
             l += lds[w * (D + 1) + D];
         }
     }
-    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+    const float inv = inverse(l);
     for (int j = 0; j < N; ++j)
         static_cast<unsigned short *>(a.out)[at * D + j * 64 + lane] = float_bits16(o[j] * inv, a.bf16);
-    if (a.lse && lane == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * 0.69314718056f;
+    if (a.lse && lane == 0) a.lse[at] = log_sum(m, l);
 }
 
 template <int D, bool FP8, int NT>
@@ -482,7 +900,7 @@ hipError_t launch(const AttendArgs &a, const AttendPlan &p, hipStream_t stream) 
     constexpr int RT = 16 * NT;
     attend_kernel<D, FP8, NT><<<(unsigned)((p.shares + 3) / 4), 256, 0, stream>>>(a);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !p.join) return e;
+    if (e != hipSuccess) return e;
     const int64_t outs = (int64_t)a.set.total * a.heads;
     // results of many parts: four waves each
     if (p.shares > 8 * p.units) join_kernel<D, RT, 4><<<(unsigned)outs, 256, 0, stream>>>(a);
@@ -490,12 +908,45 @@ hipError_t launch(const AttendArgs &a, const AttendPlan &p, hipStream_t stream) 
     return hipGetLastError();
 }
 
+template <int D, bool FP8, int NT>
+hipError_t launch_short(const AttendArgs &a, const AttendPlan &p, hipStream_t stream) {
+    constexpr int RT = 16 * NT, W = D == 256 || (D == 128 && NT == 2) ? 4 : 8;   // as many waves as have their registers at once
+    constexpr size_t lds = sizeof(float) * W * RT * (D + 4 + 2);
+    if (lds > 65536) {
+        static const hipError_t once = hipFuncSetAttribute(
+            reinterpret_cast<const void *>(attend_short_kernel<D, FP8, NT, W>),
+            hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (once != hipSuccess) return once;
+    }
+    attend_short_kernel<D, FP8, NT, W><<<(unsigned)p.units, 64 * W, lds, stream>>>(a);
+    return hipGetLastError();
+}
+
+template <int D, bool FP8, int PARTS>
+hipError_t launch_chunk(const AttendArgs &a, const AttendPlan &p, hipStream_t stream) {
+    constexpr int lds = 4 * kPage * D * 2;
+    if (lds > 65536) {
+        static const hipError_t once = hipFuncSetAttribute(
+            reinterpret_cast<const void *>(attend_chunk_kernel<D, FP8, PARTS>),
+            hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (once != hipSuccess) return once;
+    }
+    attend_chunk_kernel<D, FP8, PARTS><<<(unsigned)p.shares, 256, lds, stream>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int64_t outs = (int64_t)a.set.total * a.heads;
+    if (p.shares > 8 * p.units) join_kernel<D, 128, 4><<<(unsigned)outs, 256, 0, stream>>>(a);
+    else join_kernel<D, 128, 1><<<(unsigned)((outs + 3) / 4), 256, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
 template <int D, bool FP8>
 hipError_t pick(const AttendArgs &a, const AttendPlan &p, hipStream_t stream) {
+    if (p.tile == 128) return a.bf16 ? launch_chunk<D, FP8, 1>(a, p, stream) : launch_chunk<D, FP8, 2>(a, p, stream);
     if constexpr (D < 256) {   // at 256 two tiles do not fit the registers
-        if (p.tile == 32) return launch<D, FP8, 2>(a, p, stream);
+        if (p.tile == 32) return p.shares ? launch<D, FP8, 2>(a, p, stream) : launch_short<D, FP8, 2>(a, p, stream);
     }
-    return launch<D, FP8, 1>(a, p, stream);
+    return p.shares ? launch<D, FP8, 1>(a, p, stream) : launch_short<D, FP8, 1>(a, p, stream);
 }
 
 }  // namespace
@@ -507,19 +958,24 @@ AttendPlan attend_plan(int64_t n, int rows, int group, int kv_heads, int width, 
     const int64_t pages = len > 0 ? (len + kPage - 1) / kPage : 1;
     // query rows of one key head and table row, on average
     const int64_t mean = (n * group + rows - 1) / rows;
-    p.tile = mean > 16 && D < 256 ? 32 : 16;
+    p.tile = mean > kMany ? 128 : mean > 16 && D < 256 ? 32 : 16;
     p.units = (starts ? n * group / p.tile + rows : rows * (int64_t)((group + p.tile - 1) / p.tile)) * kv_heads;
     // as many waves as have their registers at once: 1 to 3 per SIMD
     const int64_t waves = D == 64 && p.tile == 16 ? 3072 : D == 256 || (D == 128 && p.tile == 32) ? 1024 : 2048;
-    p.shares = (int)(p.units * pages < waves ? p.units * pages : waves);
-    p.join = pages > 1;
     p.line = p.units * pages;
+    if (p.tile == 128) {
+        // as many workgroups as are resident at once: their registers, and LDS at 256
+        const int64_t groups = D == 64 ? CHUNK64 : D == 128 ? 512 : 256;
+        p.shares = (int)(p.line < groups ? p.line : groups);
+        return p;
+    }
+    p.shares = pages <= kShort && p.units <= kFew ? 0 : (int)(p.line < waves ? p.line : waves);
     return p;
 }
 
 size_t attend_info_bytes(const AttendPlan &p) { return ((size_t)p.units * 8 + 255) / 256 * 256; }
 size_t attend_bytes(const AttendPlan &p, int D) {
-    return attend_info_bytes(p) + (p.join ? sizeof(float) * 2 * (size_t)p.shares * p.tile * (D + 4) : 0);
+    return p.shares ? attend_info_bytes(p) + sizeof(float) * 2 * (size_t)p.shares * p.tile * (D + 4) : 0;
 }
 
 hipError_t kv_attend(const AttendArgs &a, const AttendPlan &p, int D, int type, hipStream_t stream) {

@@ -222,6 +222,36 @@ def test_attend_long_row(kind):
     assert torch.equal(out, cut)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_attend_chunks_of_long_rows(kind, dtype):
+    # many queries per row, each row's pages shared by many workgroups
+    lens, counts = [15011, 3, 4000], [70, 2, 33]
+    cache, rows, tables = filled(lens, 236, 310, 1, 64, kind)
+    q = torch.randn(105, 4, 64, device="cuda").to(dtype)
+    out, lse = cache.attend(0, q, tables, ints(lens), starts_of(counts), return_lse=True)
+    check_attend(cache, HostCache(cache, 0), rows, lens, q, counts, out, lse)
+
+
+def test_attend_many_rows():
+    # more rows than a wave has lanes, some of them empty, in every path
+    r = np.random.RandomState(1)
+    lens = [int(n) for n in r.randint(0, 300, 150)]
+    lens[7] = lens[149] = 0
+    lens[80] = 2000
+    cache, rows, tables = filled(lens, 32, 520, 1, 64, "int8")
+    host = HostCache(cache, 0)
+    q = torch.randn(150, 2, 64, device="cuda").to(torch.bfloat16)
+    out, lse = cache.attend(0, q, tables, ints(lens), return_lse=True)
+    check_attend(cache, host, rows, lens, q, [1] * 150, out, lse)
+    for most in (3, 60):
+        counts = [min(n, int(c)) for n, c in zip(lens, r.randint(0, most, 150))]
+        counts[3] = min(lens[3], most)
+        q = torch.randn(sum(counts), 2, 64, device="cuda").to(torch.float16)
+        out, lse = cache.attend(0, q, tables, ints(lens), starts_of(counts), return_lse=True)
+        check_attend(cache, host, rows, lens, q, counts, out, lse)
+
+
 def test_attend_queries_of_any_size():
     # float16 with one power of two per row: tiny, huge and mixed queries
     cache, rows, tables = filled([100] * 5, 2, 12, 1, 64, "int8")
@@ -242,6 +272,27 @@ def test_attend_queries_of_any_size():
     bad = cache.attend(0, q, tables, ints([100] * 5))
     assert torch.isnan(bad[0, 0]).all() and torch.isnan(bad[4, 1]).all()
     assert torch.equal(bad[1:4], out[1:4]) and torch.equal(bad[0, 1], out[0, 1]) and torch.equal(bad[4, 0], out[4, 0])
+
+
+def test_scores_past_float32s_fractions():
+    # queries so large that one key takes all: several queries of a row, in both tilings
+    cache, rows, tables = filled([90, 200], 4, 8, 1, 64, "int8")
+    host = HostCache(cache, 0)
+    for counts in ([2, 3], [60, 100]):
+        q = (torch.randn(sum(counts), 2, 64, device="cuda") * 1e18).to(torch.bfloat16)
+        out, lse = cache.attend(0, q, tables, ints([90, 200]), starts_of(counts), return_lse=True)
+        assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+        t = 0
+        for r, (n, c) in enumerate(zip([90, 200], counts)):
+            k, v = host.row(rows[r], n)
+            for i in range(c):
+                x = q[t + i].double().cpu() @ k[:n - c + i + 1, 0].T          # [heads, keys]
+                best = x.topk(2).values
+                sure = best[:, 0] - best[:, 1] > 1e-5 * best[:, 0].abs()
+                want = v[x.argmax(1), 0][sure]
+                got = out[t + i].double().cpu()[sure]
+                assert torch.all((got - want).abs() <= 2.0 ** -8 * want.abs())
+            t += c
 
 
 @pytest.mark.parametrize("kind", KINDS)
