@@ -390,7 +390,7 @@ __global__ __launch_bounds__(64 * W) void attend_short_kernel(AttendArgs a) {
 // machine evenly, and a wave has the next page's codes on the way while it
 // works, across units too.  A unit that lies in one share is written out at
 // once; of the others each share leaves a part (at most two per wave: at
-// its begin and at its end) for join_kernel.  Bound by the memory system:
+// its begin and at its end) for join kernels.  Bound by the memory system:
 // up to 16 pages of 64 D bytes in flight per compute unit.
 struct Place {                       // a page of the line; the same in all lanes
     int row, tile, kvh, page;        // page of the row
@@ -840,54 +840,97 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? LB64 : 2) void attend
     }
 }
 
-// Joins the parts of a (token, head) whose unit several shares have: W waves,
-// each takes every W-th part.
-template <int D, int RT, int W>
-__global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
-    constexpr int N = D / 64;
-    __shared__ float lds[W > 1 ? W * (D + 1) : 1];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t at = W > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
-    if (at >= (int64_t)a.set.total * a.heads) return;
+// Where a (token, head) lies among the parts; false: written already.
+template <int RT>
+__device__ inline bool find_parts(const AttendArgs &a, int64_t at, int row, int first, int count, int *place, int *parts, int *inside) {
     const int token = (int)(at / a.heads), head = (int)(at % a.heads);
+    if (token < first || token >= first + count) return false;
+    const int r = (token - first) * a.group + head % a.group;
+    const int2 info = reinterpret_cast<const int2 *>(a.info)[unit_of<RT>(a, row, first, r / RT, head / a.group)];
+    *place = info.x, *parts = info.y, *inside = r % RT;
+    // (starts that do not ascend may leave a unit without an owner)
+    return info.y > 1 && info.x >= 0 && info.y <= a.shares && (info.x & ~1) + 2 * (info.y - 1) < 2 * a.shares;
+}
+// The c-th part of a unit: the first one's place, then the first unit of each following share.
+template <int D, int RT>
+__device__ inline const float *part_of(const AttendArgs &a, int place, int inside, int c) {
+    return a.parts + ((int64_t)(c ? (place & ~1) + 2 * c : place) * RT + inside) * (D + 4);
+}
+
+// Joins the parts of the (token, head)s whose unit several shares have.
+// A few parts each: D / 4 lanes per result.
+template <int D, int RT>
+__global__ __launch_bounds__(256) void join_few_kernel(AttendArgs a) {
+    constexpr int L = D / 4;
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
+    const int64_t outs = (int64_t)a.set.total * a.heads;
+    const int d = (threadIdx.x % L) * 4;
+    const int token = (int)(min(at, outs - 1) / a.heads);
+    int row = token, first = token, count = 1;
+    if (a.set.starts) {
+        // the last row that begins at or before the token, by every thread for itself
+        int lo = 0, hi = a.set.rows - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (a.set.starts[mid] <= token) lo = mid;
+            else hi = mid - 1;
+        }
+        row = lo;
+        row_tokens(a.set.starts, row, a.set.total, &first, &count);
+    }
+    int place, parts, inside;
+    if (at >= outs || !find_parts<RT>(a, at, row, first, count, &place, &parts, &inside)) return;
+    float m = -__builtin_inff(), l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int c = 0; c < parts; ++c) {
+        const float *po = part_of<D, RT>(a, place, inside, c);
+        const f32x4 y = *reinterpret_cast<const f32x4 *>(po + d);
+        const float mc = po[D], lc = po[D + 1], mn = fmaxf(m, mc), mm = mn == -__builtin_inff() ? 0.f : mn;
+        const float e0 = __builtin_amdgcn_exp2f(m - mm), e1 = __builtin_amdgcn_exp2f(mc - mm);
+        o = o * e0 + y * e1;
+        l = l * e0 + lc * e1;
+        m = mn;
+    }
+    write4(a, at * D + d, o * inverse(l));
+    if (a.lse && d == 0) a.lse[at] = log_sum(m, l);
+}
+
+// Many parts each: a workgroup per result, each of its four waves takes every fourth part.
+template <int D, int RT>
+__global__ __launch_bounds__(256) void join_many_kernel(AttendArgs a) {
+    constexpr int N = D / 64, W = 4;
+    __shared__ float lds[W * (D + 1)];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t at = blockIdx.x;
+    const int token = (int)(at / a.heads);
     int row = token, first = token, count = 1;
     if (a.set.starts) {
         row = slot_row(a.set.starts, a.set.rows, token, 1, 1, 0);
         row_tokens(a.set.starts, row, a.set.total, &first, &count);
-        if (token < first || token >= first + count) return;
     }
-    const int r = (token - first) * a.group + head % a.group;
-    const int2 info = reinterpret_cast<const int2 *>(a.info)[unit_of<RT>(a, row, first, r / RT, head / a.group)];
-    const int place = info.x, parts = info.y;
-    if (parts <= 1) return;                          // written already
-    // (starts that do not ascend may leave a unit without an owner)
-    if (place < 0 || parts > a.shares || (place & ~1) + 2 * (parts - 1) >= 2 * a.shares) return;
-    // the first part, then the first unit of each following share
-    const float *first_part = a.parts + ((int64_t)place * RT + r % RT) * (D + 4);
-    const float *others = a.parts + ((int64_t)(place & ~1) * RT + r % RT) * (D + 4);
-    auto part_of = [&](int c) { return c ? others + (int64_t)c * 2 * RT * (D + 4) : first_part; };
+    int place, parts, inside;
+    if (!find_parts<RT>(a, at, row, first, count, &place, &parts, &inside)) return;
     float m = -__builtin_inff();
-    for (int c = lane; c < parts; c += 64) m = fmaxf(m, part_of(c)[D]);
+    for (int c = lane; c < parts; c += 64) m = fmaxf(m, part_of<D, RT>(a, place, inside, c)[D]);
     for (int k = 32; k; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
     const float mm = m == -__builtin_inff() ? 0.f : m;
     float l = 0.f, o[N];
     for (int j = 0; j < N; ++j) o[j] = 0.f;
 #pragma unroll 4
-    for (int c = W > 1 ? wave : 0; c < parts; c += W) {
-        const float *po = part_of(c);
+    for (int c = wave; c < parts; c += W) {
+        const float *po = part_of<D, RT>(a, place, inside, c);
         const float e = __builtin_amdgcn_exp2f(po[D] - mm);
         l += e * po[D + 1];
         for (int j = 0; j < N; ++j) o[j] += e * po[j * 64 + lane];
     }
-    if constexpr (W > 1) {
-        for (int j = 0; j < N; ++j) lds[wave * (D + 1) + j * 64 + lane] = o[j];
-        if (lane == 0) lds[wave * (D + 1) + D] = l;
-        __syncthreads();
-        if (wave > 0) return;
-        for (int w = 1; w < W; ++w) {
-            for (int j = 0; j < N; ++j) o[j] += lds[w * (D + 1) + j * 64 + lane];
-            l += lds[w * (D + 1) + D];
-        }
+    for (int j = 0; j < N; ++j) lds[wave * (D + 1) + j * 64 + lane] = o[j];
+    if (lane == 0) lds[wave * (D + 1) + D] = l;
+    __syncthreads();
+    if (wave > 0) return;
+    for (int w = 1; w < W; ++w) {
+        for (int j = 0; j < N; ++j) o[j] += lds[w * (D + 1) + j * 64 + lane];
+        l += lds[w * (D + 1) + D];
     }
     const float inv = inverse(l);
     for (int j = 0; j < N; ++j)
@@ -895,17 +938,20 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
     if (a.lse && lane == 0) a.lse[at] = log_sum(m, l);
 }
 
+template <int D, int RT>
+hipError_t join(const AttendArgs &a, const AttendPlan &p, hipStream_t stream) {
+    const int64_t outs = (int64_t)a.set.total * a.heads;
+    if (p.shares > 8 * p.units) join_many_kernel<D, RT><<<(unsigned)outs, 256, 0, stream>>>(a);
+    else join_few_kernel<D, RT><<<(unsigned)((outs * (D / 4) + 255) / 256), 256, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
 template <int D, bool FP8, int NT>
 hipError_t launch(const AttendArgs &a, const AttendPlan &p, hipStream_t stream) {
     constexpr int RT = 16 * NT;
     attend_kernel<D, FP8, NT><<<(unsigned)((p.shares + 3) / 4), 256, 0, stream>>>(a);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const int64_t outs = (int64_t)a.set.total * a.heads;
-    // results of many parts: four waves each
-    if (p.shares > 8 * p.units) join_kernel<D, RT, 4><<<(unsigned)outs, 256, 0, stream>>>(a);
-    else join_kernel<D, RT, 1><<<(unsigned)((outs + 3) / 4), 256, 0, stream>>>(a);
-    return hipGetLastError();
+    return e != hipSuccess ? e : join<D, RT>(a, p, stream);
 }
 
 template <int D, bool FP8, int NT>
@@ -933,11 +979,7 @@ hipError_t launch_chunk(const AttendArgs &a, const AttendPlan &p, hipStream_t st
     }
     attend_chunk_kernel<D, FP8, PARTS><<<(unsigned)p.shares, 256, lds, stream>>>(a);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const int64_t outs = (int64_t)a.set.total * a.heads;
-    if (p.shares > 8 * p.units) join_kernel<D, 128, 4><<<(unsigned)outs, 256, 0, stream>>>(a);
-    else join_kernel<D, 128, 1><<<(unsigned)((outs + 3) / 4), 256, 0, stream>>>(a);
-    return hipGetLastError();
+    return e != hipSuccess ? e : join<D, 128>(a, p, stream);
 }
 
 template <int D, bool FP8>

@@ -2,13 +2,15 @@
 //
 // Every choice (which free page goes to whom) is an exclusive prefix sum over
 // rows or page ids, so results do not depend on timing: one workgroup makes
-// it (kv_*_plan), then grids apply it to the tables and copy pages in all
-// layers.  The counters in refs are integers, so the order of their atomic
-// updates does not show.  Bound by latency (a few launches of a few
-// microseconds) for the tables and by memory for the copies.
+// it, and a grid copies pages in all layers.  Tables of ordinary size are
+// changed by the workgroup that plans (one launch before the copies: what
+// such a call costs is latency); larger ones by grids of their own
+// before and after the plan.  The counters in refs are integers, so the
+// order of their atomic updates does not show.
 #include <hip/hip_runtime.h>
 
 #include "kv.h"
+#include "lds_dma.h"
 
 namespace tq {
 namespace {
@@ -36,6 +38,11 @@ __device__ inline int block_scan(int x, int *lds, int *total) {
     return before + inc - x;
 }
 
+// A count as the atomics of this launch left it.
+__device__ inline int count_of(const int *refs, int p) {
+    return __hip_atomic_load(refs + p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
 // The ids p with refs[p] == 0 in ascending order into out, until `want` of
 // them are found or the pool ends; returns how many there are (at least min(want, all)).
 __device__ inline int list_free(const int *refs, int pages, int want, int *out, int *lds) {
@@ -45,7 +52,7 @@ __device__ inline int list_free(const int *refs, int pages, int want, int *out, 
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int p = base + threadIdx.x * 4 + j;
-            id[j] = p < pages && refs[p] == 0;
+            id[j] = p < pages && count_of(refs, p) == 0;
             n += id[j];
         }
         int all;
@@ -136,28 +143,46 @@ void launch_copy(const PagesArgs &a, const int *from, const int *to, const int *
     copy_pages_kernel<<<dim3((unsigned)x, (unsigned)along), 256, 0, stream>>>(a, from, to, count);
 }
 
-// ------------------------------------------------------------------ resize
-// A wave per row: gives back the pages past a smaller goal.
-__global__ __launch_bounds__(256) void shrink_kernel(PagesArgs a, const int *goals) {
-    const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (row >= a.rows) return;
-    const int len = min(max(a.lens[row], 0), a.width * kPage);
-    const int goal = goals[row];
-    if (goal < 0 || goal >= len) return;
-    for (int col = pages_of(goal) + lane; col < pages_of(len); col += 64) {
-        int *at = &a.tables[(int64_t)row * a.width + col];
-        const int page = *at;
-        if (page >= 0 && page < a.pages) atomicSub(&a.refs[page], 1);
-        else flag(a.cache.status, TQ_KV_BAD_PAGE);
-        *at = -1;
+// Work on ranges of columns, one range per thread of the planning workgroup:
+// a short one is its thread's, the long ones are everybody's in turn.
+struct Range {
+    int row, lo, hi, extra;          // extra: what f wants to know about the row
+};
+template <class F>
+__device__ inline void each_column(Range r, Range *big, int *bigs, F f) {
+    __syncthreads();
+    if (threadIdx.x == 0) *bigs = 0;
+    __syncthreads();
+    if (r.hi - r.lo <= 8) {
+        for (int c = r.lo; c < r.hi; ++c) f(r, c);
+    } else {
+        big[atomicAdd(bigs, 1)] = r;
     }
-    if (lane == 0) a.lens[row] = goal;
+    __syncthreads();
+    for (int i = 0; i < *bigs; ++i) {
+        const Range b = big[i];
+        for (int c = b.lo + threadIdx.x; c < b.hi; c += kPlanThreads) f(b, c);
+    }
+}
+// What this workgroup changed is seen by its later reads: stores and atomics have arrived, then the barrier.
+__device__ inline void settle() {
+    wait_vmem<0>();
+    __syncthreads();
 }
 
-// One workgroup: how many pages each growing row asks for and where they
-// begin in the list of free ones; that list.
-__global__ __launch_bounds__(kPlanThreads) void resize_plan_kernel(PagesArgs a, const int *goals) {
-    __shared__ int lds[kPlanThreads / 64];
+// ------------------------------------------------------------------ resize
+__device__ inline void give_back(const PagesArgs &a, int row, int col) {
+    int *at = &a.tables[(int64_t)row * a.width + col];
+    const int page = *at;
+    if (page >= 0 && page < a.pages) atomicSub(&a.refs[page], 1);
+    else flag(a.cache.status, TQ_KV_BAD_PAGE);
+    *at = -1;
+}
+__device__ inline int row_len(const PagesArgs &a, int row) { return min(max(a.lens[row], 0), a.width * kPage); }
+
+// How many pages the growing rows ask for and where they begin in the list
+// of free ones; that list.  By one workgroup.
+__device__ inline void plan_resize(const PagesArgs &a, const int *goals, int *lds) {
     const Scratch s = scratch(a.ws, a.pages, a.rows, 0);
     int total = 0, copies = 0;
     for (int base = 0; base < a.rows; base += kPlanThreads) {
@@ -165,7 +190,7 @@ __global__ __launch_bounds__(kPlanThreads) void resize_plan_kernel(PagesArgs a, 
         int more = 0;
         bool shared = false;
         if (row < a.rows) {
-            const int len = min(max(a.lens[row], 0), a.width * kPage), goal = goals[row];
+            const int len = row_len(a, row), goal = goals[row];
             if (goal > len) {
                 if (goal > a.width * kPage) {
                     flag(a.cache.status, TQ_KV_FULL);
@@ -173,7 +198,7 @@ __global__ __launch_bounds__(kPlanThreads) void resize_plan_kernel(PagesArgs a, 
                     more = pages_of(goal) - pages_of(len);
                     if (len % kPage) {
                         const int page = a.tables[(int64_t)row * a.width + len / kPage];
-                        if (page >= 0 && page < a.pages) shared = a.refs[page] > 1;
+                        if (page >= 0 && page < a.pages) shared = count_of(a.refs, page) > 1;
                         else flag(a.cache.status, TQ_KV_BAD_PAGE);
                     }
                     more += shared;
@@ -200,36 +225,88 @@ __global__ __launch_bounds__(kPlanThreads) void resize_plan_kernel(PagesArgs a, 
     }
 }
 
-// A wave per row: takes its pages.
+// What a growing row gets: columns [lo, hi) from fresh[extra] on (none: lo = hi).
+// With `lead` also the row's length, and the copy of a shared page.
+__device__ inline Range taken(const PagesArgs &a, const int *goals, int row, bool lead) {
+    const Scratch s = scratch(a.ws, a.pages, a.rows, 0);
+    const int len = row_len(a, row), goal = goals[row];
+    if (goal <= len || goal > a.width * kPage) return {row, 0, 0, 0};
+    const bool shared = s.more[row] & kCopied;
+    const int more = s.more[row] & ~kCopied, begin = s.begin[row];
+    if (more > 0 && (int64_t)begin + more > s.head[0]) {
+        if (lead) {
+            flag(a.cache.status, TQ_KV_FULL);
+            if (shared) s.from[s.place[row]] = -1;
+        }
+        return {row, 0, 0, 0};
+    }
+    const int first = pages_of(len) - (shared ? 1 : 0);
+    if (lead) {
+        if (shared) {
+            const int old = a.tables[(int64_t)row * a.width + first];
+            atomicSub(&a.refs[old], 1);
+            s.from[s.place[row]] = old;
+            s.to[s.place[row]] = s.fresh[begin];
+        }
+        a.lens[row] = goal;
+    }
+    return {row, first, first + more, begin - first};
+}
+__device__ inline void put_page(const PagesArgs &a, const int *fresh, const Range &r, int col) {
+    const int page = fresh[r.extra + col];
+    a.refs[page] = 1;
+    a.tables[(int64_t)r.row * a.width + col] = page;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void resize_kernel(PagesArgs a, const int *goals) {
+    __shared__ int lds[kPlanThreads / 64], bigs;
+    __shared__ Range big[kPlanThreads];
+    const Scratch s = scratch(a.ws, a.pages, a.rows, 0);
+    for (int base = 0; base < a.rows; base += kPlanThreads) {
+        const int row = base + threadIdx.x;
+        Range r = {row, 0, 0, 0};
+        int goal = -1;
+        if (row < a.rows) {
+            const int len = row_len(a, row);
+            goal = goals[row];
+            if (goal >= 0 && goal < len) r = {row, pages_of(goal), pages_of(len), 0};
+            else goal = -1;
+        }
+        each_column(r, big, &bigs, [&](const Range &b, int c) { give_back(a, b.row, c); });
+        if (goal >= 0) a.lens[row] = goal;
+    }
+    settle();
+    plan_resize(a, goals, lds);
+    settle();
+    for (int base = 0; base < a.rows; base += kPlanThreads) {
+        const int row = base + threadIdx.x;
+        const Range r = row < a.rows ? taken(a, goals, row, true) : Range{row, 0, 0, 0};
+        each_column(r, big, &bigs, [&](const Range &b, int c) { put_page(a, s.fresh, b, c); });
+    }
+}
+
+// The same with a wave per row around the plan.
+__global__ __launch_bounds__(256) void shrink_kernel(PagesArgs a, const int *goals) {
+    const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (row >= a.rows) return;
+    const int len = row_len(a, row), goal = goals[row];
+    if (goal < 0 || goal >= len) return;
+    for (int col = pages_of(goal) + lane; col < pages_of(len); col += 64) give_back(a, row, col);
+    if (lane == 0) a.lens[row] = goal;
+}
+__global__ __launch_bounds__(kPlanThreads) void resize_plan_kernel(PagesArgs a, const int *goals) {
+    __shared__ int lds[kPlanThreads / 64];
+    plan_resize(a, goals, lds);
+}
 __global__ __launch_bounds__(256) void grow_kernel(PagesArgs a, const int *goals) {
     const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (row >= a.rows) return;
     const Scratch s = scratch(a.ws, a.pages, a.rows, 0);
-    const int len = min(max(a.lens[row], 0), a.width * kPage), goal = goals[row];
-    if (goal <= len || goal > a.width * kPage) return;
-    const bool shared = s.more[row] & kCopied;
-    const int more = s.more[row] & ~kCopied, begin = s.begin[row];
-    if (more > 0 && (int64_t)begin + more > s.head[0]) {
-        if (lane == 0) {
-            flag(a.cache.status, TQ_KV_FULL);
-            if (shared) s.from[s.place[row]] = -1;
-        }
-        return;
-    }
-    int *table = a.tables + (int64_t)row * a.width;
-    const int first = pages_of(len) - (shared ? 1 : 0);
-    if (shared && lane == 0) {
-        const int old = table[first];
-        atomicSub(&a.refs[old], 1);
-        s.from[s.place[row]] = old;
-        s.to[s.place[row]] = s.fresh[begin];
-    }
-    for (int j = lane; j < more; j += 64) {
-        const int page = s.fresh[begin + j];
-        a.refs[page] = 1;
-        table[first + j] = page;
-    }
-    if (lane == 0) a.lens[row] = goal;
+    // all lanes look before the first one changes the row
+    Range r = taken(a, goals, row, false);
+    __builtin_amdgcn_wave_barrier();
+    if (lane == 0) taken(a, goals, row, true);
+    for (int col = r.lo + lane; col < r.hi; col += 64) put_page(a, s.fresh, r, col);
 }
 
 // -------------------------------------------------------------------- fork
@@ -239,15 +316,14 @@ __device__ inline bool pair_rows(const PagesArgs &a, const int *src, const int *
     return *from != *to && *from >= 0 && *from < a.rows && *to >= 0 && *to < a.rows;
 }
 
-__global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(PagesArgs a, const int *src, const int *dst, int n) {
-    __shared__ int lds[kPlanThreads / 64];
+// Which pairs need a page for their part-filled last one; the free pages.
+__device__ inline void plan_fork(const PagesArgs &a, const int *src, const int *dst, int n, int *lds) {
     const Scratch s = scratch(a.ws, a.pages, a.rows, n);
     int total = 0;
     for (int base = 0; base < n; base += kPlanThreads) {
         const int i = base + threadIdx.x;
         int part = 0, from, to;
-        if (i < n && pair_rows(a, src, dst, i, &from, &to))
-            part = min(max(a.lens[from], 0), a.width * kPage) % kPage != 0;
+        if (i < n && pair_rows(a, src, dst, i, &from, &to)) part = row_len(a, from) % kPage != 0;
         int all;
         const int at = total + block_scan(part, lds, &all);
         if (i < n) {
@@ -263,27 +339,25 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(PagesArgs a, co
     }
 }
 
-// A wave per pair: the new row into the workspace, before any row changes.
-__global__ __launch_bounds__(256) void fork_stage_kernel(PagesArgs a, const int *src, const int *dst, int n) {
-    const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (i >= n) return;
+// `lanes` threads per pair: the new row into the workspace, before any row changes.
+__device__ inline void stage_pair(const PagesArgs &a, const int *src, const int *dst, int n, int i, int lane, int lanes) {
     const Scratch s = scratch(a.ws, a.pages, a.rows, n);
     int from, to;
     if (!pair_rows(a, src, dst, i, &from, &to)) return;
-    const int len = min(max(a.lens[from], 0), a.width * kPage);
+    const int len = row_len(a, from);
     const bool part = s.more[i], fits = !part || s.begin[i] < s.head[0];
     const int whole = fits ? len / kPage : 0;
     const int *table = a.tables + (int64_t)from * a.width;
-    for (int col = lane; col < a.width; col += 64) s.stage[(int64_t)i * a.width + col] = col < whole ? table[col] : -1;
+    const int page = part && fits ? s.fresh[s.begin[i]] : -1;
+    for (int col = lane; col < a.width; col += lanes)
+        s.stage[(int64_t)i * a.width + col] = col < whole ? table[col] : col == whole ? page : -1;
     if (lane == 0) {
         s.slens[i] = fits ? len : 0;
         if (!fits) flag(a.cache.status, TQ_KV_FULL);
         if (part) {
             int old = -1;
             if (fits) {
-                const int page = s.fresh[s.begin[i]];
                 old = table[whole];
-                s.stage[(int64_t)i * a.width + whole] = page;
                 s.to[s.begin[i]] = page;
                 if (old < 0 || old >= a.pages) {
                     old = -1;
@@ -295,14 +369,12 @@ __global__ __launch_bounds__(256) void fork_stage_kernel(PagesArgs a, const int 
     }
 }
 
-__global__ __launch_bounds__(256) void fork_apply_kernel(PagesArgs a, const int *src, const int *dst, int n) {
-    const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (i >= n) return;
+__device__ inline void apply_pair(const PagesArgs &a, const int *src, const int *dst, int n, int i, int lane, int lanes) {
     const Scratch s = scratch(a.ws, a.pages, a.rows, n);
     int from, to;
     if (!pair_rows(a, src, dst, i, &from, &to)) return;
     int *table = a.tables + (int64_t)to * a.width;
-    for (int col = lane; col < a.width; col += 64) {
+    for (int col = lane; col < a.width; col += lanes) {
         const int old = table[col], page = s.stage[(int64_t)i * a.width + col];
         if (old >= 0 && old < a.pages) atomicSub(&a.refs[old], 1);
         if (page >= 0 && page < a.pages) atomicAdd(&a.refs[page], 1);   // a fresh one: 0 -> 1
@@ -311,9 +383,32 @@ __global__ __launch_bounds__(256) void fork_apply_kernel(PagesArgs a, const int 
     if (lane == 0) a.lens[to] = s.slens[i];
 }
 
-// ----------------------------------------------------------------- compact
-__global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(PagesArgs a, int *live_out) {
+__global__ __launch_bounds__(kPlanThreads) void fork_kernel(PagesArgs a, const int *src, const int *dst, int n) {
     __shared__ int lds[kPlanThreads / 64];
+    constexpr int kLanes = 16;
+    const int group = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+    plan_fork(a, src, dst, n, lds);
+    settle();
+    for (int i = group; i < n; i += kPlanThreads / kLanes) stage_pair(a, src, dst, n, i, lane, kLanes);
+    settle();
+    for (int i = group; i < n; i += kPlanThreads / kLanes) apply_pair(a, src, dst, n, i, lane, kLanes);
+}
+
+__global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(PagesArgs a, const int *src, const int *dst, int n) {
+    __shared__ int lds[kPlanThreads / 64];
+    plan_fork(a, src, dst, n, lds);
+}
+__global__ __launch_bounds__(256) void fork_stage_kernel(PagesArgs a, const int *src, const int *dst, int n) {
+    const int i = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (i < n) stage_pair(a, src, dst, n, i, threadIdx.x & 63, 64);
+}
+__global__ __launch_bounds__(256) void fork_apply_kernel(PagesArgs a, const int *src, const int *dst, int n) {
+    const int i = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (i < n) apply_pair(a, src, dst, n, i, threadIdx.x & 63, 64);
+}
+
+// ----------------------------------------------------------------- compact
+__device__ inline void plan_compact(const PagesArgs &a, int *live_out, int *lds) {
     const Scratch s = scratch(a.ws, a.pages, a.rows, 0);
     int live = 0;
     for (int base = 0; base < a.pages; base += kPlanThreads * 4) {
@@ -361,11 +456,12 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(PagesArgs a,
     }
 }
 
-__global__ __launch_bounds__(256) void compact_apply_kernel(PagesArgs a) {
+// Tables and counts after the moves: cells and moves `first`, first + step, ...
+__device__ inline void apply_compact(const PagesArgs &a, int64_t first, int64_t step) {
     const Scratch s = scratch(a.ws, a.pages, a.rows, 0);
     const int live = s.head[2], moves = s.head[1];
-    const int64_t cells = (int64_t)a.rows * a.width, step = (int64_t)gridDim.x * 256;
-    for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < cells; i += step) {
+    const int64_t cells = (int64_t)a.rows * a.width;
+    for (int64_t i = first; i < cells; i += step) {
         const int page = a.tables[i];
         if (page >= live && page < a.pages) {
             const int m = s.fresh[page];
@@ -374,11 +470,28 @@ __global__ __launch_bounds__(256) void compact_apply_kernel(PagesArgs a) {
             else flag(a.cache.status, TQ_KV_BAD_PAGE);
         }
     }
-    for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < moves; i += step) {
+    for (int64_t i = first; i < moves; i += step) {
         a.refs[s.to[i]] = a.refs[s.from[i]];
         a.refs[s.from[i]] = 0;
     }
 }
+
+__global__ __launch_bounds__(kPlanThreads) void compact_kernel(PagesArgs a, int *live_out) {
+    __shared__ int lds[kPlanThreads / 64];
+    plan_compact(a, live_out, lds);
+    settle();
+    apply_compact(a, threadIdx.x, kPlanThreads);
+}
+__global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(PagesArgs a, int *live_out) {
+    __shared__ int lds[kPlanThreads / 64];
+    plan_compact(a, live_out, lds);
+}
+__global__ __launch_bounds__(256) void compact_apply_kernel(PagesArgs a) {
+    apply_compact(a, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
+}
+
+// Where one workgroup changes the tables itself.
+constexpr int kOneRows = 4096, kOneCells = 32768, kOneForked = 16384;
 
 }  // namespace
 
@@ -388,31 +501,43 @@ size_t kv_rows_bytes(int64_t pages, int64_t rows, int64_t width, int64_t n) {
 }
 
 hipError_t kv_resize(const PagesArgs &a, const int *goals, hipStream_t stream) {
-    const unsigned grid = (unsigned)((a.rows + 3) / 4);
     const Scratch s = scratch(a.ws, a.pages, a.rows, 0);
-    shrink_kernel<<<grid, 256, 0, stream>>>(a, goals);
-    resize_plan_kernel<<<1, kPlanThreads, 0, stream>>>(a, goals);
-    grow_kernel<<<grid, 256, 0, stream>>>(a, goals);
+    if (a.rows <= kOneRows) {
+        resize_kernel<<<1, kPlanThreads, 0, stream>>>(a, goals);
+    } else {
+        const unsigned grid = (unsigned)((a.rows + 3) / 4);
+        shrink_kernel<<<grid, 256, 0, stream>>>(a, goals);
+        resize_plan_kernel<<<1, kPlanThreads, 0, stream>>>(a, goals);
+        grow_kernel<<<grid, 256, 0, stream>>>(a, goals);
+    }
     launch_copy(a, s.from, s.to, s.head + 1, a.rows, stream);
     return hipGetLastError();
 }
 
 hipError_t kv_fork(const PagesArgs &a, const int *src, const int *dst, int n, hipStream_t stream) {
-    const unsigned grid = (unsigned)((n + 3) / 4);
     const Scratch s = scratch(a.ws, a.pages, a.rows, n);
-    fork_plan_kernel<<<1, kPlanThreads, 0, stream>>>(a, src, dst, n);
-    fork_stage_kernel<<<grid, 256, 0, stream>>>(a, src, dst, n);
-    fork_apply_kernel<<<grid, 256, 0, stream>>>(a, src, dst, n);
+    if ((int64_t)n * a.width <= kOneForked) {
+        fork_kernel<<<1, kPlanThreads, 0, stream>>>(a, src, dst, n);
+    } else {
+        const unsigned grid = (unsigned)((n + 3) / 4);
+        fork_plan_kernel<<<1, kPlanThreads, 0, stream>>>(a, src, dst, n);
+        fork_stage_kernel<<<grid, 256, 0, stream>>>(a, src, dst, n);
+        fork_apply_kernel<<<grid, 256, 0, stream>>>(a, src, dst, n);
+    }
     launch_copy(a, s.from, s.to, s.head + 1, n, stream);
     return hipGetLastError();
 }
 
 hipError_t kv_compact(const PagesArgs &a, int *live, hipStream_t stream) {
     const Scratch s = scratch(a.ws, a.pages, a.rows, 0);
-    const int64_t cells = (int64_t)a.rows * a.width > a.pages ? (int64_t)a.rows * a.width : a.pages;
-    compact_plan_kernel<<<1, kPlanThreads, 0, stream>>>(a, live);
-    const unsigned grid = (unsigned)(cells / 256 + 1 < 1024 ? cells / 256 + 1 : 1024);
-    compact_apply_kernel<<<grid, 256, 0, stream>>>(a);
+    if ((int64_t)a.rows * a.width <= kOneCells) {
+        compact_kernel<<<1, kPlanThreads, 0, stream>>>(a, live);
+    } else {
+        const int64_t cells = (int64_t)a.rows * a.width > a.pages ? (int64_t)a.rows * a.width : a.pages;
+        compact_plan_kernel<<<1, kPlanThreads, 0, stream>>>(a, live);
+        const unsigned grid = (unsigned)(cells / 256 + 1 < 1024 ? cells / 256 + 1 : 1024);
+        compact_apply_kernel<<<grid, 256, 0, stream>>>(a);
+    }
     launch_copy(a, s.from, s.to, s.head + 1, a.pages, stream);
     return hipGetLastError();
 }

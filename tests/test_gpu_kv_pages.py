@@ -109,6 +109,28 @@ def test_many_rows_and_pages():
     b.compact()
 
 
+def test_tables_that_grids_change():
+    # over 4,096 rows and 32,768 entries, rows of one to eight pages
+    r = np.random.RandomState(5)
+    b = Both(5003, 8, 24000, layers=1)
+    b.resize(r.randint(0, 500, 5003).tolist())
+    b.resize([int(n) if r.rand() < 0.6 else 3 for n in r.randint(-90, 512, 5003)])
+    b.fork(r.randint(0, 5003, 4200).tolist(), r.permutation(5003)[:4200].tolist())
+    b.resize([max(0, n - int(r.randint(0, 70))) for n in b.host.lens])
+    b.resize([n + int(r.randint(0, 9)) for n in b.host.lens])
+    b.compact()
+
+
+def test_long_rows():
+    # many columns at once: the ranges that the whole workgroup takes
+    b = Both(5, 300, 1100, layers=1)
+    b.resize([19200, 5, 9000, 0, 700])
+    b.fork([0, 2], [3, 1])
+    b.resize([0, 12000, 64, 100, -1])
+    b.resize([10000, 0, 19200, 101, 0])
+    b.compact()
+
+
 def test_empty_calls():
     b = Both(2, 2, 4)
     b.fork([], [])
