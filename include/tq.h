@@ -539,8 +539,9 @@ tq_status tq_kv_compact(const tq_kv_rows *rows, const tq_kv_cache *cache,
  * packed rows [n_keys][kv_heads][head_dim], all of `dtype`; starts_dev and
  * key_starts_dev [rows + 1] (NULL: as starts_dev).  causal: query i of a row
  * of m queries and l keys sees the keys 0..i + l - m, else all l.  out and
- * lse as in tq_kv_attend.  head_dim 64, 128 or 256.  `longest` bounds the
- * queries of a row (0: n).  float32 sums and statistics; the weights are
+ * lse as in tq_kv_attend.  head_dim 64, 128 or 256.  `longest` (0: not known)
+ * is the most queries of a row: short rows need less preparation if
+ * they are known to be.  float32 sums and statistics; the weights are
  * rounded to `dtype`. */
 tq_status tq_attention(const tq_rows *q, const tq_rows *k, const tq_rows *v,
                        int32_t dtype, int64_t n, int64_t n_keys, int32_t heads,

@@ -67,10 +67,12 @@ struct PromptArgs {
     int64_t qt, qh, kt, kh, vt, vh;
     const int *starts, *key_starts;
     int rows, total, keys, heads, group, kv_heads, causal, wide;
+    int levels;                   // tiles of the longest row where all are short, else 0
     float scale2;
     void *out;
     float *lse;
 };
+int prompt_levels(int group, int longest);
 hipError_t prompt_attention(const PromptArgs &a, int D, int bf16, hipStream_t stream);
 
 struct PagesArgs {

@@ -294,7 +294,7 @@ tq_status tq_attention(const tq_rows *q, const tq_rows *k, const tq_rows *v, int
         if (rows == 0 || !starts) return fail(TQ_EINVAL, "queries but no rows, or starts is NULL");
         if (!out || (reinterpret_cast<uintptr_t>(out) & 7)) return fail(TQ_EINVAL, "out is NULL or not 8-byte aligned");
         const int group = heads / kv_heads;
-        if ((n * group / 32 + rows) * kv_heads >= kMostGroups || n * group > kMost)
+        if ((n * group / 32 + 4 * (int64_t)rows) * kv_heads >= kMostGroups || n * group > kMost)
             return fail(TQ_EUNSUPPORTED, "too many queries for one call");
         if ((st = device_ready()) != TQ_OK) return st;
         PromptArgs a;
@@ -310,6 +310,7 @@ tq_status tq_attention(const tq_rows *q, const tq_rows *k, const tq_rows *v, int
         a.heads = heads;
         a.group = group;
         a.kv_heads = kv_heads;
+        a.levels = prompt_levels(group, longest);
         a.causal = causal;
         a.wide = wide_rows(q) && wide_rows(k) && wide_rows(v);
         a.scale2 = scale * 1.44269504089f;

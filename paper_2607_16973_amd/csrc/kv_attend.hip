@@ -769,31 +769,40 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? LB64 : 2) void attend
                 for (int d = 0; d < DT; ++d) o[d] *= back;
                 m = m1;
                 mv = m2;
-                wild = __any(fabsf(m1) > 0x1p20f && m1 > -__builtin_inff());
+                wild = __any(fabsf(m1) > 0x1p8f && m1 > -__builtin_inff());
             }
+            // Weight and value scale in one exponent, 2^(s f - m) 2^gain; the sum
+            // takes the gain back, once per block.  A block without a value scale has codes of 0 and may
+            // have any; one of 2^-60 and less rounds to 0 next to the largest.
             const float m1 = m == -__builtin_inff() ? 0.f : m, m2 = mv == -__builtin_inff() ? 0.f : mv;
-            float shift = -m1;
-            if (wild) {   // products and maximum rounded alike: the largest score gives 0
+            float gain[4], shift[4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                gain[b] = vlog[b] == -__builtin_inff() ? kUnit : fminf(fmaxf(vlog[b] + (m1 - m2) + kUnit, -60.f), 126.f);
+                shift[b] = gain[b] - m1;
+            }
+            if (wild) {   // a maximum whose fractions float32 rounds off: scores relative to it first
 #pragma unroll
                 for (int j = 0; j < 32; ++j) s[j >> 4][j & 15] = scaled_less(s[j >> 4][j & 15], f[j >> 3], m1);
-                for (int b = 0; b < 4; ++b) f[b] = 1.f;
-                shift = 0.f;
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    f[b] = 1.f;
+                    shift[b] = gain[b];
+                }
             }
-            float sum[2] = {0.f, 0.f};
             f16x8 w[4], wl[PARTS > 1 ? 4 : 1];
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-                const float gain = __builtin_amdgcn_exp2f(fminf(vlog[b] + (m1 - m2) + kUnit, 126.f));
+                float sum[2] = {0.f, 0.f};
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b >> 1][8 * (b & 1) + i], f[b], shift));
-                    sum[i & 1] += e;
-                    const float y = e * gain;
+                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b >> 1][8 * (b & 1) + i], f[b], shift[b]));
+                    sum[i & 1] += y;
                     w[b][i] = (_Float16)y;
                     if constexpr (PARTS > 1) wl[b][i] = (_Float16)(y - (float)w[b][i]);
                 }
+                l += (sum[0] + sum[1]) * __builtin_amdgcn_exp2f(-gain[b]);
             }
-            l += sum[0] + sum[1];
 #pragma unroll
             for (int b = 0; b < 4; ++b)
 #pragma unroll

@@ -11,11 +11,13 @@
 
 #include "kv.h"
 #include "lds_dma.h"
+#include "stream.h"
 
 namespace tq {
 namespace {
 
 constexpr int kPlanThreads = 1024;
+constexpr int kOneForked = 32;      // pairs that the planning workgroup forks itself, 32 threads each
 
 // Exclusive prefix sum over the workgroup's threads; *total receives the sum.
 __device__ inline int block_scan(int x, int *lds, int *total) {
@@ -113,24 +115,28 @@ __global__ __launch_bounds__(256) void copy_pages_kernel(PagesArgs a, const int 
     const int64_t base = (int64_t)layer * a.cache.pages;
     char *codes = (which ? a.cache.v : a.cache.k) + (int64_t)piece * kPiece;
     const int n = (int)(min(store - (int64_t)piece * kPiece, (int64_t)kPiece) / 16);
+    int src = from[blockIdx.x], dst = to[blockIdx.x];
     for (int i = blockIdx.x; i < count; i += gridDim.x) {
-        const int src = from[i], dst = to[i];
-        if (src < 0) continue;
-        const uint4 *s = reinterpret_cast<const uint4 *>(codes + (base + src) * store);
-        uint4 *d = reinterpret_cast<uint4 *>(codes + (base + dst) * store);
-        uint4 x[4];
+        const int next = i + gridDim.x < count ? i + gridDim.x : i, next_src = from[next], next_dst = to[next];
+        if (src >= 0) {
+            const u32x4 *s = reinterpret_cast<const u32x4 *>(codes + (base + src) * store);
+            u32x4 *d = reinterpret_cast<u32x4 *>(codes + (base + dst) * store);
+            u32x4 x[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j * 256 + (int)threadIdx.x < n) x[j] = s[j * 256 + threadIdx.x];
+            for (int j = 0; j < 4; ++j)
+                if (j * 256 + (int)threadIdx.x < n) x[j] = __builtin_nontemporal_load(s + j * 256 + threadIdx.x);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j * 256 + (int)threadIdx.x < n) d[j * 256 + threadIdx.x] = x[j];
-        if (piece == 0) {
-            float *sc = which ? a.cache.vs : a.cache.ks;
-            const int64_t row = (int64_t)a.cache.heads * 4;
-            for (int j = threadIdx.x; j < (int)row; j += 256)
-                sc[(base + dst) * row + j] = sc[(base + src) * row + j];
+            for (int j = 0; j < 4; ++j)
+                if (j * 256 + (int)threadIdx.x < n) __builtin_nontemporal_store(x[j], d + j * 256 + threadIdx.x);
+            if (piece == 0) {
+                float *sc = which ? a.cache.vs : a.cache.ks;
+                const int64_t row = (int64_t)a.cache.heads * 4;
+                for (int j = threadIdx.x; j < (int)row; j += 256)
+                    sc[(base + dst) * row + j] = sc[(base + src) * row + j];
+            }
         }
+        src = next_src;
+        dst = next_dst;
     }
 }
 
@@ -385,13 +391,13 @@ __device__ inline void apply_pair(const PagesArgs &a, const int *src, const int 
 
 __global__ __launch_bounds__(kPlanThreads) void fork_kernel(PagesArgs a, const int *src, const int *dst, int n) {
     __shared__ int lds[kPlanThreads / 64];
-    constexpr int kLanes = 16;
+    constexpr int kLanes = kPlanThreads / kOneForked;
     const int group = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
     plan_fork(a, src, dst, n, lds);
     settle();
-    for (int i = group; i < n; i += kPlanThreads / kLanes) stage_pair(a, src, dst, n, i, lane, kLanes);
+    if (group < n) stage_pair(a, src, dst, n, group, lane, kLanes);
     settle();
-    for (int i = group; i < n; i += kPlanThreads / kLanes) apply_pair(a, src, dst, n, i, lane, kLanes);
+    if (group < n) apply_pair(a, src, dst, n, group, lane, kLanes);
 }
 
 __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(PagesArgs a, const int *src, const int *dst, int n) {
@@ -491,7 +497,7 @@ __global__ __launch_bounds__(256) void compact_apply_kernel(PagesArgs a) {
 }
 
 // Where one workgroup changes the tables itself.
-constexpr int kOneRows = 4096, kOneCells = 32768, kOneForked = 16384;
+constexpr int kOneRows = 4096, kOneCells = 32768;
 
 }  // namespace
 
@@ -516,7 +522,7 @@ hipError_t kv_resize(const PagesArgs &a, const int *goals, hipStream_t stream) {
 
 hipError_t kv_fork(const PagesArgs &a, const int *src, const int *dst, int n, hipStream_t stream) {
     const Scratch s = scratch(a.ws, a.pages, a.rows, n);
-    if ((int64_t)n * a.width <= kOneForked) {
+    if (n <= kOneForked) {
         fork_kernel<<<1, kPlanThreads, 0, stream>>>(a, src, dst, n);
     } else {
         const unsigned grid = (unsigned)((n + 3) / 4);

@@ -104,7 +104,8 @@ def attention(q, k, v, starts, key_starts=None, *, causal=True, scale=None, long
     bounds each row's queries, key_starts its keys (None: the same).  causal:
     the last query sees every key of its row, each one before it one key
     less; a query that sees none gives 0.  scale: 1/sqrt(d) by default.
-    longest: the most queries of a row where the caller knows it.
+    longest: the most queries of a row where the caller knows it (short rows
+    then start sooner).
     Returns out [n, heads, d], with return_lse also the float32 [n, heads]
     logarithm of each query's sum (-inf where it sees no key)."""
     shape = _dims(q, 3, "q")

@@ -141,6 +141,16 @@ def test_repeats_are_equal_and_streams():
     assert got.data_ptr() == out.data_ptr() and torch.equal(out, first)
 
 
+def test_longest_is_a_hint():
+    counts = [700, 3, 0, 129, 1500]
+    q, k, v = (rows(counts, h, 64, torch.float16, 80 + h) for h in (6, 2, 3))
+    v = v[:, :2]
+    st = starts_of(counts)
+    want = tq.attention(q, k, v, st)
+    for longest in (1500, 2000, 1499, 700, 40, 1):
+        assert torch.equal(tq.attention(q, k, v, st, longest=longest), want)
+
+
 def test_graph():
     counts = [64, 17]
     q, k, v = (rows(counts, 4, 64, torch.float16, 60 + s) for s in range(3))
