@@ -58,11 +58,13 @@ __device__ inline float max3(float a, float b, float c) {
     return r;
 }
 
-// Piece of a row at which piece c of key row kr lies.
+// Piece of a row at which piece c of key row kr lies.  The banks repeat every
+// 16 pieces (256 bytes): 16 neighbouring key rows are read at one c, four
+// value rows at four neighbouring c, and both times all 16 differ.
 template <int CH>
-__device__ inline int k_piece(int kr, int c) { return c ^ (kr & (CH - 1) & 15); }
+__device__ inline int k_piece(int kr, int c) { return CH == 8 ? c ^ ((kr >> 1) & 7) : c ^ (kr & 15); }
 template <int CH>
-__device__ inline int v_piece(int kr, int c) { return c ^ ((kr & (CH / 2 - 1) & 7) << 1); }
+__device__ inline int v_piece(int kr, int c) { return CH == 8 ? c ^ ((kr >> 1 & 1) << 2) : c ^ ((kr & 3) << 2); }
 
 // Transposing LDS read: of 16 lanes, lane 4 j + c names 4 coordinates (8 bytes) of
 // key j; lane i receives coordinate i of the four keys.
@@ -136,19 +138,27 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void prompt_kernel(PromptArg
     }
 
     // The rows of a step into half `to` of LDS; past the last key its row
-    // again (its scores are masked).
+    // again (its scores are masked).  A lane's pieces are a fixed distance from the step's first row.
     const unsigned short *kbase = static_cast<const unsigned short *>(a.k) + (int64_t)kfirst * a.kt + (int64_t)kvh * a.kh;
     const unsigned short *vbase = static_cast<const unsigned short *>(a.v) + (int64_t)kfirst * a.vt + (int64_t)kvh * a.vh;
+    uint32_t koff[CH / 4], voff[CH / 4];
+    auto offsets = [&](int most) {                        // rows up to `most` of a step
+#pragma unroll
+        for (int i = 0; i < CH / 4; ++i) {
+            const int at = (i * 4 + wave) * 64 + lane, kr = at / CH, p = at % CH, key = min(kr, most);
+            koff[i] = (uint32_t)key * (uint32_t)(2 * a.kt) + k_piece<CH>(kr, p) * 16;
+            voff[i] = (uint32_t)key * (uint32_t)(2 * a.vt) + v_piece<CH>(kr, p) * 16;
+        }
+    };
     auto stage = [&](int k0, int to) {
         if constexpr (WIDE) {
+            if (k0 + kKeys > keys) offsets(keys - 1 - k0);
+            const unsigned short *ks = kbase + (int64_t)k0 * a.kt, *vs = vbase + (int64_t)k0 * a.vt;
 #pragma unroll
             for (int i = 0; i < CH / 4; ++i) {            // 64 pieces each: kKeys * CH / 256 of a wave
-                const int first_piece = (i * 4 + wave) * 64, at = first_piece + lane;
-                const int kr = at / CH, p = at % CH, key = min(k0 + kr, keys - 1);
-                const unsigned short *ks = kbase + key * a.kt + k_piece<CH>(kr, p) * 8;
-                const unsigned short *vs = vbase + key * a.vt + v_piece<CH>(kr, p) * 8;
-                lds_dma16(ks, lds0 + to * 2 * TILE + first_piece * 16);
-                lds_dma16(vs, lds0 + to * 2 * TILE + TILE + first_piece * 16);
+                const uint32_t to_lds = lds0 + to * 2 * TILE + (i * 4 + wave) * 1024;
+                lds_dma16_s(koff[i], ks, to_lds);
+                lds_dma16_s(voff[i], vs, to_lds + TILE);
             }
         } else {
             for (int at = threadIdx.x; at < kKeys * CH; at += 256) {
@@ -182,6 +192,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void prompt_kernel(PromptArg
             vat[d] = lds0 + TILE + (kr * CH + v_piece<CH>(kr, d * 4 + ((lane >> 4) & 1) * 2 + ((s & 3) >> 1))) * 16 + (s & 1) * 8;
     }
 
+    if constexpr (WIDE) offsets(kKeys);
     if (steps) stage(0, 0);
     for (int step = 0; step < steps; ++step) {
         const int k0 = step * kKeys;
@@ -319,7 +330,10 @@ hipError_t launch(const PromptArgs &a, hipStream_t stream) {
 template <int D, bool BF16>
 hipError_t pick(const PromptArgs &a, hipStream_t stream) {
     if (!a.wide) return launch<D, BF16, false, false>(a, stream);
-    return a.levels ? launch<D, BF16, true, true>(a, stream) : launch<D, BF16, true, false>(a, stream);
+    if constexpr (D < 256) {   // at 256 the loop over tiles takes registers that are not there
+        if (a.levels) return launch<D, BF16, true, true>(a, stream);
+    }
+    return launch<D, BF16, true, false>(a, stream);
 }
 template <int D>
 hipError_t pick(const PromptArgs &a, int bf16, hipStream_t stream) {

@@ -198,7 +198,7 @@ tq_status tq_kv_attend(const tq_kv_cache *cache, int32_t layer, const tq_rows *q
         const size_t need = attend_bytes(p, cache->head_dim);
         if (need && (!ws || ws_bytes < need || !aligned16(ws)))
             return fail(TQ_EINVAL, "workspace too small or not aligned");
-        if (p.line > kMost || p.units >= kMostGroups / 2 || n * heads >= kMostGroups || n * group > kMost)
+        if (p.line >= (int64_t)1 << 30 || p.units >= kMostGroups / 2 || n * heads >= kMostGroups || n * group > kMost)
             return fail(TQ_EUNSUPPORTED, "too many queries or tokens for one call");
         if ((st = device_ready()) != TQ_OK) return st;
         AttendArgs a;
@@ -312,7 +312,8 @@ tq_status tq_attention(const tq_rows *q, const tq_rows *k, const tq_rows *v, int
         a.kv_heads = kv_heads;
         a.levels = prompt_levels(group, longest);
         a.causal = causal;
-        a.wide = wide_rows(q) && wide_rows(k) && wide_rows(v);
+        // a step's 64 rows lie within 32-bit distances
+        a.wide = wide_rows(q) && wide_rows(k) && wide_rows(v) && k->token_stride < 1 << 24 && v->token_stride < 1 << 24;
         a.scale2 = scale * 1.44269504089f;
         a.out = out;
         a.lse = lse;

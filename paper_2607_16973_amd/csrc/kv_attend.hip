@@ -28,6 +28,7 @@
 namespace tq {
 namespace {
 
+constexpr int kLine = 1 << 30;    // pages of all units together stay below
 constexpr float kUnit = 6.f;      // weights are held in units of 2^-kUnit ...
 constexpr float kLag = 8.f;       // ... and may pass the running maximum by 2^kLag before it follows
 
@@ -42,16 +43,8 @@ __device__ inline float max3(float a, float b, float c) {
 // 64 rows of 500 to 1,500 (512 units); with 2,048 units the even shares are ahead (88 us against 70),
 // and so are they from 46 pages on (25.6 against 20.4 for one row of 2,900).
 constexpr int kShort = 24, kFew = 512;
-#ifndef CHUNK64
-#define CHUNK64 768
-#endif
-#ifndef LB64
-#define LB64 3
-#endif
-#ifndef MANY
-#define MANY 48
-#endif
-constexpr int kMany = MANY;
+// Above so many query rows per key head and table row the chunked kernel.
+constexpr int kMany = 48;
 
 // 16 codes -> 2 x 8 float16.
 template <bool FP8>
@@ -447,40 +440,38 @@ __device__ inline int64_t unit_of(const AttendArgs &a, int row, int first, int t
 template <int RT>
 __device__ inline bool find_share(const AttendArgs &a, int share, int *each, int *x, int *end, Place *cur) {
     const int lane = __lane_id(), heads = a.layer.heads;
-    auto pages_at = [&](int row) {
-        Place p;
-        if (row >= a.set.rows) return 0;
-        row_shape<RT>(a, row, &p);
-        return p.tiles * p.pages * heads;
-    };
-    auto running = [&](int v) {                      // inclusive sum over the lanes
-        for (int k = 1; k < 64; k <<= 1) {
-            const int y = __shfl_up(v, k);
-            if (lane >= k) v += y;
+    // 64 stretches of rows at a time, a lane each, then those of the stretch
+    // that x lies in: one round for up to 64 rows, two for up to 4,096.  Sums
+    // stop at kLine, which only starts that do not ascend can reach: then
+    // nothing is done.
+    int lo = 0, count = a.set.rows, before = 0;
+    for (bool whole = true;; whole = false) {
+        const int part = (count + 63) >> 6, from = lane * part, to = min(from + part, count);
+        int sums = 0;
+        for (int i = from; i < to; ++i) {
+            Place p;
+            row_shape<RT>(a, lo + i, &p);
+            sums = (int)min(sums + (int64_t)p.tiles * p.pages * heads, (int64_t)kLine);
         }
-        return v;
-    };
-    int total = 0, sums = 0;
-    for (int base = 0; base < a.set.rows; base += 64) {
-        sums = running(pages_at(base + lane));
-        total += __builtin_amdgcn_readlane(sums, 63);
-    }
-    *each = (total + a.shares - 1) / a.shares;
-    *x = share * *each;
-    *end = min(*x + *each, total);
-    if (*x >= *end) return false;
-    int before = 0;
-    for (int base = 0;; base += 64) {
-        if (a.set.rows > 64) sums = running(pages_at(base + lane));
-        const uint64_t past = __ballot(before + sums > *x);
-        if (past) {
-            const int at = __builtin_ctzll(past);
-            if (at) before += __builtin_amdgcn_readlane(sums, at - 1);
-            to_row<RT>(a, base + at, cur);
-            break;
+        for (int k = 1; k < 64; k <<= 1) {           // inclusive sums over the lanes
+            const int y = __shfl_up(sums, k);
+            if (lane >= k) sums = min(sums + y, kLine);
         }
-        before += __builtin_amdgcn_readlane(sums, 63);
+        if (whole) {
+            const int total = __builtin_amdgcn_readlane(sums, 63);
+            if (total >= kLine) return false;
+            *each = (total + a.shares - 1) / a.shares;
+            *x = share * *each;
+            *end = min(*x + *each, total);
+            if (*x >= *end) return false;
+        }
+        const int at = __builtin_ctzll(__ballot(before + sums > *x));
+        if (at) before += __builtin_amdgcn_readlane(sums, at - 1);
+        lo += at * part;
+        count = min(part, count - at * part);
+        if (count <= 1) break;
     }
+    to_row<RT>(a, __builtin_amdgcn_readfirstlane(lo), cur);
     const int within = *x - before, unit = within / cur->pages;
     cur->page = within % cur->pages;
     cur->tile = unit / heads;
@@ -592,7 +583,7 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendArgs a) {
 // to the product in that many float16 parts (two for float16 results, whose
 // own rounding is as small as that of the weights).
 template <int D, bool FP8, int PARTS>
-__global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? LB64 : 2) void attend_chunk_kernel(AttendArgs a) {
+__global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void attend_chunk_kernel(AttendArgs a) {
     constexpr int KS = D / 16, DT = D / 32, CH = D / 8, RT = 128, RAW = D / 64;
     constexpr int TILE = kPage * D * 2;              // bytes of a page's keys in float16
     extern __shared__ __align__(16) char store[];    // [2][keys [64][D], values [D][64]]
@@ -643,7 +634,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? LB64 : 2) void attend
             const int c = threadIdx.x + i * 256;
             f16x8 lo, hi;
             to_half<FP8>(kraw[i], &lo, &hi);
-            const int kr = c / (D / 16), p = 2 * (c % (D / 16)), swap = kr & (CH - 1) & 15;
+            const int kr = c / (D / 16), p = 2 * (c % (D / 16)), swap = CH == 8 ? (kr >> 1) & 7 : kr & 15;
             *reinterpret_cast<f16x8 *>(base + (kr * CH + (p ^ swap)) * 16) = lo;
             *reinterpret_cast<f16x8 *>(base + (kr * CH + ((p + 1) ^ swap)) * 16) = hi;
             to_half<FP8>(vraw[i], &lo, &hi);
@@ -721,7 +712,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? LB64 : 2) void attend
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const int kr = t * 32 + n;
-                    const f16x8 k = *reinterpret_cast<const f16x8 *>(half + (kr * CH + ((2 * c + h) ^ (kr & (CH - 1) & 15))) * 16);
+                    const f16x8 k = *reinterpret_cast<const f16x8 *>(half + (kr * CH + ((2 * c + h) ^ (CH == 8 ? (kr >> 1) & 7 : kr & 15))) * 16);
                     s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[c], s[t], 0, 0, 0);
                 }
         }
@@ -1016,7 +1007,7 @@ AttendPlan attend_plan(int64_t n, int rows, int group, int kv_heads, int width, 
     p.line = p.units * pages;
     if (p.tile == 128) {
         // as many workgroups as are resident at once: their registers, and LDS at 256
-        const int64_t groups = D == 64 ? CHUNK64 : D == 128 ? 512 : 256;
+        const int64_t groups = D == 64 ? 768 : D == 128 ? 512 : 256;
         p.shares = (int)(p.line < groups ? p.line : groups);
         return p;
     }
