@@ -43,8 +43,10 @@ __device__ inline float max3(float a, float b, float c) {
 // 64 rows of 500 to 1,500 (512 units); with 2,048 units the even shares are ahead (88 us against 70),
 // and so are they from 46 pages on (25.6 against 20.4 for one row of 2,900).
 constexpr int kShort = 24, kFew = 512;
-// Above so many query rows per key head and table row the chunked kernel.
-constexpr int kMany = 48;
+// Above so many query rows per key head and table row the chunked kernel: at
+// 56 (8 heads of 7 tokens, three rows of up to 61,049 tokens, d = 128) 118 us against 152
+// with four tiles of 16 rows to a wave, at 30 119 us against 138 the other way round.
+constexpr int kMany = 32;
 
 // 16 codes -> 2 x 8 float16.
 template <bool FP8>
@@ -202,7 +204,7 @@ __device__ inline void page_step(Rows<D, NT> &t, Page<D> &page, int index, int l
     next_keys();
     __builtin_amdgcn_sched_barrier(0);
     const int base = index * kPage + 16 * g;         // position of the lane's first token
-    float vlog = page.vs > 0.f ? __log2f(page.vs) : -__builtin_inff();
+    float vlog = page.vs > 0.f ? __builtin_amdgcn_logf(page.vs) : -__builtin_inff();
     // A page that holds the row's end may hold anything past it: those
     // codes and scales are taken out before they meet a zero weight.
     if ((index + 1) * kPage > len || !here) {
@@ -526,7 +528,6 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendArgs a) {
             open = false;
         }
         const bool more = at + 1 < end;
-        const Place then = next;
         page_step<D, FP8, NT>(t, page, cur.page, len, g, [&] {
             if (!more) return;
             tile = take(a, page, __builtin_amdgcn_readfirstlane(ahead), any_in(a, next), next.kvh);
@@ -569,7 +570,7 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendArgs a) {
             if (from == 0 && lane == 0) tell_parts<RT>(a, cur, at, each, place);
             open = true;
         }
-        cur = then;
+        if (more) advance<RT>(a, &cur);
     }
 }
 
@@ -717,12 +718,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void attend_ch
                 }
         }
         const Coming now = here;
-        const Place then = next;
         if (at + 1 < end) {
             put((at - x + 1) & 1);
             here = coming;
             if (at + 2 < end) {
-                next = after;
+                advance<RT>(a, &next);
                 load(next, __builtin_amdgcn_readfirstlane(ahead));
                 if (at + 3 < end) {
                     advance<RT>(a, &after);
@@ -742,7 +742,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void attend_ch
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 f[b] = fmaxf(factor * now.ks[b], 0x1p-126f);   // never 0: a masked score stays -inf
-                vlog[b] = now.vs[b] > 0.f ? __log2f(now.vs[b]) : -__builtin_inff();
+                vlog[b] = now.vs[b] > 0.f ? __builtin_amdgcn_logf(now.vs[b]) : -__builtin_inff();
                 float big = max3(s[b >> 1][8 * (b & 1)], s[b >> 1][8 * (b & 1) + 1], s[b >> 1][8 * (b & 1) + 2]);
                 big = max3(big, s[b >> 1][8 * (b & 1) + 3], s[b >> 1][8 * (b & 1) + 4]);
                 big = max3(big, s[b >> 1][8 * (b & 1) + 5], s[b >> 1][8 * (b & 1) + 6]);
@@ -836,7 +836,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void attend_ch
             if (from == 0 && threadIdx.x == 0) tell_parts<RT>(a, cur, at, each, place);
             open = true;
         }
-        cur = then;
+        if (at + 1 < end) advance<RT>(a, &cur);
     }
 }
 
