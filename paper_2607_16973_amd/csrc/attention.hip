@@ -236,8 +236,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void prompt_kernel(PromptArg
 #pragma unroll
         for (int j = 3; j < 31; j += 2) big = max3(big, s[j >> 4][j & 15], s[(j + 1) >> 4][(j + 1) & 15]);
         big = max_of_halves(fmaxf(big, s[1][15]));
-        if (__any((big - m) * c2 > kLag || (m == -__builtin_inff() && big > m))) {
-            const float mn = fmaxf(m, big), mm = mn == -__builtin_inff() ? 0.f : mn;
+        const bool over = (big - m) * c2 > kLag || (m == -__builtin_inff() && big > m);
+        if (__any(over)) {   // each row by itself, so that none depends on its neighbours
+            const float mn = over ? fmaxf(m, big) : m, mm = mn == -__builtin_inff() ? 0.f : mn;
             const float alpha = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m - mm) * c2);
             l *= alpha;
 #pragma unroll

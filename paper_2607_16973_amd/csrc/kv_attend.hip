@@ -230,8 +230,9 @@ __device__ inline void page_step(Rows<D, NT> &t, Page<D> &page, int index, int l
         for (int j = 3; j < 15; j += 2) big = max3(big, s[i][j >> 2][j & 3], s[i][(j + 1) >> 2][(j + 1) & 3]);
         big = fmaxf(big, s[i][3][3]) * f;
         const float top1 = max_of_groups(big), top2 = max_of_groups(big + vlog);
-        if (__any(top1 > t.m[i] + kLag || top2 > t.mv[i] + kLag)) {
-            const float m1 = fmaxf(t.m[i], top1), m2 = fmaxf(t.mv[i], top2);
+        const bool over = top1 > t.m[i] + kLag || top2 > t.mv[i] + kLag;
+        if (__any(over)) {   // each row by itself, so that none depends on its neighbours
+            const float m1 = over ? fmaxf(t.m[i], top1) : t.m[i], m2 = over ? fmaxf(t.mv[i], top2) : t.mv[i];
             t.l[i] *= t.m[i] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(t.m[i] - m1);
             const float back = t.mv[i] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(t.mv[i] - m2);
 #pragma unroll
@@ -752,8 +753,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void attend_ch
             }
             top1 = max_of_halves(top1);
             top2 = max_of_halves(top2);
-            if (__any(top1 > m + kLag || top2 > mv + kLag)) {
-                const float m1 = fmaxf(m, top1), m2 = fmaxf(mv, top2);
+            const bool over = top1 > m + kLag || top2 > mv + kLag;
+            if (__any(over)) {   // each row by itself, so that none depends on its neighbours
+                const float m1 = over ? fmaxf(m, top1) : m, m2 = over ? fmaxf(mv, top2) : mv;
                 l *= m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - m1);
                 const float back = mv == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(mv - m2);
 #pragma unroll

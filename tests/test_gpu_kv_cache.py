@@ -233,6 +233,18 @@ def test_attend_chunks_of_long_rows(kind, dtype):
     check_attend(cache, HostCache(cache, 0), rows, lens, q, counts, out, lse)
 
 
+@pytest.mark.parametrize("counts", [[1, 1], [6, 9], [100, 200]])
+def test_attend_rows_do_not_depend_on_each_other(counts):
+    lens = [1900, 300]
+    cache, rows, tables = filled(lens, 30, 40, 1, 64, "int8")
+    g = torch.Generator(device="cuda").manual_seed(11)
+    q = torch.randn(sum(counts), 4, 64, generator=g, device="cuda").to(torch.float16)
+    want = cache.attend(0, q, tables, ints(lens), starts_of(counts))
+    q[:, 2] *= 30
+    out = cache.attend(0, q, tables, ints(lens), starts_of(counts))
+    assert torch.equal(out[:, [0, 1, 3]], want[:, [0, 1, 3]])
+
+
 def test_attend_many_rows():
     # more rows than a wave has lanes, some of them empty, in every path
     r = np.random.RandomState(1)

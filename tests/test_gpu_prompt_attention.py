@@ -141,6 +141,18 @@ def test_repeats_are_equal_and_streams():
     assert got.data_ptr() == out.data_ptr() and torch.equal(out, first)
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_rows_do_not_depend_on_each_other(dtype):
+    # scores of one head far above the others': their results stay the same bits
+    counts = [300]
+    q, k, v = (rows(counts, h, 64, dtype, 90 + s) for s, h in enumerate((4, 1, 1)))
+    want = tq.attention(q, k, v, starts_of(counts))
+    q2 = q.clone()
+    q2[:, 1] *= 20
+    out = tq.attention(q2, k, v, starts_of(counts))
+    assert torch.equal(out[:, [0, 2, 3]], want[:, [0, 2, 3]])
+
+
 def test_longest_is_a_hint():
     counts = [700, 3, 0, 129, 1500]
     q, k, v = (rows(counts, h, 64, torch.float16, 80 + h) for h in (6, 2, 3))
