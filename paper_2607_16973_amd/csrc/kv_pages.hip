@@ -17,7 +17,6 @@ namespace tq {
 namespace {
 
 constexpr int kPlanThreads = 1024;
-constexpr int kOneForked = 32;      // pairs that the planning workgroup forks itself, 32 threads each
 
 // Exclusive prefix sum over the workgroup's threads; *total receives the sum.
 __device__ inline int block_scan(int x, int *lds, int *total) {
@@ -345,26 +344,22 @@ __device__ inline void plan_fork(const PagesArgs &a, const int *src, const int *
     }
 }
 
-// `lanes` threads per pair: the new row into the workspace, before any row changes.
-__device__ inline void stage_pair(const PagesArgs &a, const int *src, const int *dst, int n, int i, int lane, int lanes) {
+// The whole pages that pair i shares with row `from`, and the page of its
+// part-filled rest (-1: none).  With `lead` also its length and its copy.
+__device__ inline int new_row(const PagesArgs &a, int n, int i, int from, bool lead, int *rest) {
     const Scratch s = scratch(a.ws, a.pages, a.rows, n);
-    int from, to;
-    if (!pair_rows(a, src, dst, i, &from, &to)) return;
     const int len = row_len(a, from);
     const bool part = s.more[i], fits = !part || s.begin[i] < s.head[0];
     const int whole = fits ? len / kPage : 0;
-    const int *table = a.tables + (int64_t)from * a.width;
-    const int page = part && fits ? s.fresh[s.begin[i]] : -1;
-    for (int col = lane; col < a.width; col += lanes)
-        s.stage[(int64_t)i * a.width + col] = col < whole ? table[col] : col == whole ? page : -1;
-    if (lane == 0) {
+    *rest = part && fits ? s.fresh[s.begin[i]] : -1;
+    if (lead) {
         s.slens[i] = fits ? len : 0;
         if (!fits) flag(a.cache.status, TQ_KV_FULL);
         if (part) {
             int old = -1;
             if (fits) {
-                old = table[whole];
-                s.to[s.begin[i]] = page;
+                old = a.tables[(int64_t)from * a.width + whole];
+                s.to[s.begin[i]] = *rest;
                 if (old < 0 || old >= a.pages) {
                     old = -1;
                     flag(a.cache.status, TQ_KV_BAD_PAGE);
@@ -373,44 +368,93 @@ __device__ inline void stage_pair(const PagesArgs &a, const int *src, const int 
             s.from[s.begin[i]] = old;
         }
     }
+    return whole;
+}
+// A cell of a table gets another page.
+__device__ inline void exchange(const PagesArgs &a, int64_t cell, int was, int now) {
+    if (was >= 0 && was < a.pages) atomicSub(&a.refs[was], 1);
+    if (now >= 0 && now < a.pages) atomicAdd(&a.refs[now], 1);   // a fresh one: 0 -> 1
+    a.tables[cell] = now;
 }
 
-__device__ inline void apply_pair(const PagesArgs &a, const int *src, const int *dst, int n, int i, int lane, int lanes) {
-    const Scratch s = scratch(a.ws, a.pages, a.rows, n);
-    int from, to;
-    if (!pair_rows(a, src, dst, i, &from, &to)) return;
-    int *table = a.tables + (int64_t)to * a.width;
-    for (int col = lane; col < a.width; col += lanes) {
-        const int old = table[col], page = s.stage[(int64_t)i * a.width + col];
-        if (old >= 0 && old < a.pages) atomicSub(&a.refs[old], 1);
-        if (page >= 0 && page < a.pages) atomicAdd(&a.refs[page], 1);   // a fresh one: 0 -> 1
-        table[col] = page;
-    }
-    if (lane == 0) a.lens[to] = s.slens[i];
-}
-
+// All of it by the planning workgroup: a thread per pair, then threads over
+// the cells of all new rows, four at a time so that their loads overlap.
 __global__ __launch_bounds__(kPlanThreads) void fork_kernel(PagesArgs a, const int *src, const int *dst, int n) {
     __shared__ int lds[kPlanThreads / 64];
-    constexpr int kLanes = kPlanThreads / kOneForked;
-    const int group = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+    __shared__ int4 pairs[kPlanThreads];              // from (-1: none), to, whole pages, the page of the rest
+    const Scratch s = scratch(a.ws, a.pages, a.rows, n);
     plan_fork(a, src, dst, n, lds);
     settle();
-    if (group < n) stage_pair(a, src, dst, n, group, lane, kLanes);
+    const int mine = threadIdx.x;
+    if (mine < n) {
+        int4 p;
+        if (pair_rows(a, src, dst, mine, &p.x, &p.y)) {
+            p.z = new_row(a, n, mine, p.x, true, &p.w);
+        } else {
+            p.x = -1;
+        }
+        pairs[mine] = p;
+    }
+    __syncthreads();
+    const int cells = n * a.width, step = 4 * kPlanThreads;
+    for (int base = threadIdx.x; base < cells; base += step) {
+        int x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = base + j * kPlanThreads, at = i / a.width, col = i % a.width;
+            if (i >= cells) continue;
+            const int4 p = pairs[at];
+            x[j] = p.x < 0 ? -1 : col < p.z ? a.tables[(int64_t)p.x * a.width + col] : col == p.z ? p.w : -1;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (base + j * kPlanThreads < cells) s.stage[base + j * kPlanThreads] = x[j];
+    }
     settle();
-    if (group < n) apply_pair(a, src, dst, n, group, lane, kLanes);
+    for (int base = threadIdx.x; base < cells; base += step) {
+        int was[4], now[4], to[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = base + j * kPlanThreads, at = i / a.width;
+            to[j] = -1;
+            if (i >= cells) continue;
+            const int4 p = pairs[at];
+            if (p.x < 0) continue;
+            to[j] = p.y * a.width + i % a.width;
+            was[j] = a.tables[to[j]];
+            now[j] = s.stage[i];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (to[j] >= 0) exchange(a, to[j], was[j], now[j]);
+    }
+    if (mine < n && pairs[mine].x >= 0) a.lens[pairs[mine].y] = s.slens[mine];
 }
 
 __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(PagesArgs a, const int *src, const int *dst, int n) {
     __shared__ int lds[kPlanThreads / 64];
     plan_fork(a, src, dst, n, lds);
 }
+// A wave per pair: the new row into the workspace, before any row changes.
 __global__ __launch_bounds__(256) void fork_stage_kernel(PagesArgs a, const int *src, const int *dst, int n) {
-    const int i = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (i < n) stage_pair(a, src, dst, n, i, threadIdx.x & 63, 64);
+    const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    int from, to, rest;
+    if (i >= n || !pair_rows(a, src, dst, i, &from, &to)) return;
+    const Scratch s = scratch(a.ws, a.pages, a.rows, n);
+    const int whole = new_row(a, n, i, from, lane == 0, &rest);
+    for (int col = lane; col < a.width; col += 64)
+        s.stage[(int64_t)i * a.width + col] = col < whole ? a.tables[(int64_t)from * a.width + col] : col == whole ? rest : -1;
 }
 __global__ __launch_bounds__(256) void fork_apply_kernel(PagesArgs a, const int *src, const int *dst, int n) {
-    const int i = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (i < n) apply_pair(a, src, dst, n, i, threadIdx.x & 63, 64);
+    const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    int from, to;
+    if (i >= n || !pair_rows(a, src, dst, i, &from, &to)) return;
+    const Scratch s = scratch(a.ws, a.pages, a.rows, n);
+    for (int col = lane; col < a.width; col += 64) {
+        const int64_t cell = (int64_t)to * a.width + col;
+        exchange(a, cell, a.tables[cell], s.stage[(int64_t)i * a.width + col]);
+    }
+    if (lane == 0) a.lens[to] = s.slens[i];
 }
 
 // ----------------------------------------------------------------- compact
@@ -496,8 +540,11 @@ __global__ __launch_bounds__(256) void compact_apply_kernel(PagesArgs a) {
     apply_compact(a, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
 }
 
-// Where one workgroup changes the tables itself.
-constexpr int kOneRows = 4096, kOneCells = 32768;
+// Where one workgroup changes the tables itself: rows (resize: 512 rows up and
+// down 26 us against 38 with grids), cells of the tables (compact), cells of the new rows
+// (fork: 7,680 of them 41 us against 37 with grids; up to two per thread a launch's
+// worth less).
+constexpr int kOneRows = 4096, kOneCells = 32768, kOneForked = 2048;
 
 }  // namespace
 
@@ -522,7 +569,7 @@ hipError_t kv_resize(const PagesArgs &a, const int *goals, hipStream_t stream) {
 
 hipError_t kv_fork(const PagesArgs &a, const int *src, const int *dst, int n, hipStream_t stream) {
     const Scratch s = scratch(a.ws, a.pages, a.rows, n);
-    if (n <= kOneForked) {
+    if (n <= kPlanThreads && (int64_t)n * a.width <= kOneForked) {
         fork_kernel<<<1, kPlanThreads, 0, stream>>>(a, src, dst, n);
     } else {
         const unsigned grid = (unsigned)((n + 3) / 4);

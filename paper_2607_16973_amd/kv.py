@@ -302,13 +302,17 @@ class KVPages:
                                 _on(refs, (pages,), _I32, index, "refs"), pages, rows, width)
         _gpu(tables, "tables")
         self.tables, self.lens, self.refs = tables, lens, refs
+        self._ws = None   # kept: calls on the same rows follow one another anyway
         self._index, self._ref = index, _ref(self._view)
 
     def _workspace(self, n: int, cache):
         if cache._index != self._index or _current_device() != self._index:
             raise ValueError("the rows, the cache and the current device must be one GPU")
         v = self._view
-        return self.lens.new_empty((_pages_bytes(v.pages, v.rows, v.width, n),), dtype=torch.uint8)
+        need = _pages_bytes(v.pages, v.rows, v.width, n)
+        if self._ws is None or self._ws.numel() < need:
+            self._ws = self.lens.new_empty((need,), dtype=torch.uint8)
+        return self._ws
 
     def resize(self, goals, cache: KVCache) -> None:
         """Sets the rows' lengths to goals (int32 [rows], negative: leave):

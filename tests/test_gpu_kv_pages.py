@@ -121,6 +121,16 @@ def test_tables_that_grids_change():
     b.compact()
 
 
+@pytest.mark.parametrize("rows,width", [(1100, 1), (60, 34), (61, 34), (300, 9)])
+def test_forks_around_the_limits_of_one_workgroup(rows, width):
+    # 1,024 pairs and 2,048 cells
+    r = np.random.RandomState(rows)
+    b = Both(rows, width, rows * width + 50, layers=1)
+    b.resize(r.randint(0, width * 64 // 2 + 1, rows).tolist())
+    for n in (rows, rows - 1, min(rows, 1024)):
+        b.fork(r.randint(0, rows, n).tolist(), r.permutation(rows)[:n].tolist())
+
+
 def test_long_rows():
     # many columns at once: the ranges that the whole workgroup takes
     b = Both(5, 300, 1100, layers=1)
