@@ -23,7 +23,9 @@
 // the same card).  The matrix cores are busy half of the time and vector
 // instructions (32 exponentials, 130 others per step) the other half, at a
 // clock of 2.0 GHz: taking vector instructions out (no maximum per step), raising
-// the products' priority and interleaving both by hand were all slower.
+// the products' priority and interleaving both by hand were all slower.  At
+// d = 64 three waves per SIMD (687 TFLOP/s for 8,001 tokens) are ahead of two (575) and of
+// four that spill (595).
 #include <hip/hip_runtime.h>
 
 #include "kv.h"
@@ -89,7 +91,7 @@ __device__ inline u32x2 read_transposed(uint32_t at) {
 // than kShortTiles: the row needs no search.  Rows that are longer than that all the same are
 // gone through in strides of a.levels tiles.
 template <int D, bool BF16, bool WIDE, bool SHORT>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void prompt_kernel(PromptArgs a) {
+__global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void prompt_kernel(PromptArgs a) {
     typedef typename Half<BF16>::x8 x8;
     constexpr int KS = D / 16, DT = D / 32, CH = D / 8;   // CH: 16-byte pieces of a row
     constexpr int TILE = kKeys * D * 2;                   // bytes of a step's keys

@@ -343,6 +343,79 @@ def test_bad_page_ids_are_left_out():
         cache.check()
 
 
+@pytest.mark.parametrize("counts", [[1, 1], [3, 50]])
+def test_offsets_past_32_bits(counts):
+    # pages at the far end of a 9 GB cache: the same results as in a small one
+    lens, heads, d = [200, 130], 8, 128
+    small, rows, tables = filled(lens, 4, 8, heads, d, "int8")
+    far = 70000
+    big = tq.KVCache(1, far, heads, d, "int8")
+    assert far * heads * 64 * d > 2 ** 32
+    moved = torch.where(tables >= 0, far - 8 + tables, tables)
+    new = new_values(lens, heads, d, torch.float16, 100)
+    big.append(0, new[0], new[1], moved, ints(lens), starts_of(lens))
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q = torch.randn(sum(counts), 16, d, generator=g, device="cuda").to(torch.bfloat16)
+    args = (ints(lens), None if counts == [1, 1] else starts_of(counts))
+    assert torch.equal(big.attend(0, q, moved, *args), small.attend(0, q, tables, *args))
+    # and a page copied from one end to the other
+    state = tq.KVPages(2, 4, far)
+    state.tables[0] = moved[0]
+    state.lens[0] = 200
+    state.refs[moved[0].long()] = 1
+    state.fork(ints([0]), ints([1]), big)
+    assert state.tables[1].tolist() == moved[0, :3].tolist() + [0]
+    assert torch.equal(big.k[0, 0], big.k[0, moved[0, 3]]) and torch.equal(big.v_scale[0, 0, :, 0], big.v_scale[0, moved[0, 3], :, 0])
+
+
+def test_calls_on_another_stream():
+    cache, rows, tables = filled([300, 40], 5, 12, 2, 64, "fp8")
+    lens = ints([301, 41])
+    new = new_values([1, 1], 2, 64, torch.float16, 14)
+    q = torch.randn(2, 4, 64, device="cuda").to(torch.float16)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        cache.append(0, new[0], new[1], tables, lens)
+        out, lse = cache.attend(0, q, tables, lens, return_lse=True)
+    torch.cuda.current_stream().wait_stream(side)
+    check_attend(cache, HostCache(cache, 0), rows, [301, 41], q, [1, 1], out, lse)
+
+
+def test_refusals_of_the_binding():
+    cache, rows, tables = filled([30], 2, 3, 2, 64, "int8")
+    q = torch.randn(1, 4, 64, device="cuda").to(torch.float16)
+    lens = ints([30])
+    with pytest.raises(ValueError):
+        cache.attend(0, q[:, :, :32], tables, lens)
+    with pytest.raises(TypeError):
+        cache.attend(0, q.float(), tables, lens)
+    with pytest.raises(TypeError):
+        cache.attend(0, q, tables.long(), lens)
+    with pytest.raises(ValueError):
+        cache.attend(0, q, tables, ints([30, 1]))
+    with pytest.raises(ValueError):
+        cache.attend(0, q, tables.expand(2, 2).t()[:1], lens)
+    with pytest.raises(ValueError):
+        cache.attend(0, q.transpose(1, 2).contiguous().transpose(1, 2), tables, lens)
+    with pytest.raises(ValueError):
+        cache.attend(0, q, tables, lens, out=torch.empty(1, 4, 64, device="cuda", dtype=torch.float16)[:, :2])
+    with pytest.raises(TypeError):
+        cache.attend(0, q, tables.cpu(), lens)
+    with pytest.raises(tq.TQError):
+        cache.attend(1, q, tables, lens)
+    with pytest.raises(tq.TQError):
+        cache.attend(0, q[:, :3], tables, lens)
+    with pytest.raises(tq.TQError):
+        cache.attend(0, q, torch.zeros(1, 2000, dtype=torch.int32, device="cuda"), lens, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(ValueError):
+        cache.append(0, q, q, tables, lens)
+    with pytest.raises(ValueError):
+        tq.KVPages(1, 2, 3).fork(ints([0]), ints([0, 0]), cache)
+    with pytest.raises(tq.TQError):
+        tq.KVPages(1, 2, 4).compact(cache)
+
+
 def test_graph_of_a_step():
     cache, rows, tables = filled([100, 40], 3, 8, 2, 64, "int8")
     lens = ints([101, 41])
