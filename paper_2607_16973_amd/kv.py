@@ -24,11 +24,13 @@ _current_device = torch._C._cuda_getDevice
 
 def _on(t, shape, dtype, index, name):
     """The address of a contiguous tensor of this shape and type on GPU `index`."""
-    if not (isinstance(t, torch.Tensor) and t.shape == shape and t.dtype is dtype and t.get_device() == index
-            and t.is_contiguous()):
-        _refuse(t, shape, dtype, index, name)
-        raise ValueError("%s must be contiguous" % name)
-    return t.data_ptr()
+    try:
+        if t.shape == shape and t.dtype is dtype and t.get_device() == index and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:   # no tensor
+        pass
+    _refuse(t, shape, dtype, index, name)
+    raise ValueError("%s must be contiguous" % name)
 
 
 def _refuse(t, shape, dtype, index, name):
@@ -46,12 +48,15 @@ def _refuse(t, shape, dtype, index, name):
 
 def _packed(t, shape, dtype, index, name):
     """tq_rows of packed vectors; strides are free except the last."""
-    if not (isinstance(t, torch.Tensor) and t.shape == shape and t.dtype is dtype and t.get_device() == index):
-        _refuse(t, shape, dtype, index, name)
-    a, b, c = t.stride()
-    if c != 1:
-        raise ValueError("%s: the last dimension must be contiguous" % name)
-    return RowsView(t.data_ptr(), a, b)
+    try:
+        if t.shape == shape and t.dtype is dtype and t.get_device() == index:
+            a, b, c = t.stride()
+            if c == 1:
+                return RowsView(t.data_ptr(), a, b)
+    except AttributeError:
+        pass
+    _refuse(t, shape, dtype, index, name)
+    raise ValueError("%s: the last dimension must be contiguous" % name)
 
 
 def _dims(t, ndim, name):
@@ -194,10 +199,19 @@ class KVCache:
                                  _on(v_scale, blocks, _F32, index, "v_scale"),
                                  None if status is None else _on(status, (1,), _I32, index, "status"),
                                  pages, layers, heads, d, KV_TYPES[name])
-        _gpu(k, "k")
+        if index < 0 or index != _current_device():
+            _gpu(k, "k")   # says why not
         self.k, self.v, self.k_scale, self.v_scale, self.status = k, v, k_scale, v_scale, status
-        self.layers, self.pages, self.kv_heads, self.head_dim, self.dtype = layers, pages, heads, d, name
-        self._index, self._ref = index, _ref(self._view)
+        self.kv_heads, self.head_dim, self.dtype, self._index = heads, d, name, index
+        self._ref = _ref(self._view)
+
+    @property
+    def layers(self) -> int:
+        return self._view.layers
+
+    @property
+    def pages(self) -> int:
+        return self._view.pages
 
     @property
     def device(self):
