@@ -261,10 +261,12 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void prompt_ke
         float c1 = c2, s1 = shift;
         if (wild) {   // both products rounded alike: the largest score gives 0
             const float mm = m == -__builtin_inff() ? 0.f : m * c2;
+            if (fabsf(mm) > 0x1p20f) {   // (a row for itself)
 #pragma unroll
-            for (int j = 0; j < 32; ++j) s[j >> 4][j & 15] = scaled_less(s[j >> 4][j & 15], c2, mm);
-            c1 = 1.f;
-            s1 = Half<BF16>::kBias;
+                for (int j = 0; j < 32; ++j) s[j >> 4][j & 15] = scaled_less(s[j >> 4][j & 15], c2, mm);
+                c1 = 1.f;
+                s1 = Half<BF16>::kBias;
+            }
         }
         typename Half<BF16>::x1 pw[32];
         float sum[2] = {0.f, 0.f};

@@ -20,7 +20,8 @@
 // log2(value scale), so that weights times value scales stay in float16's
 // range whatever the scales are; they are taken to the product in two
 // float16 parts (22 bits: the product is far from its limit here, and the rounding of the weights
-// would otherwise be as large as that of a float16 result).
+// would otherwise be as large as that of a float16 result).  (The chunked kernel, which is
+// bound by its instructions, has one reference for both.)
 #include <hip/hip_runtime.h>
 
 #include "kv.h"
@@ -672,7 +673,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void attend_ch
     }
 
     f16x8 q[KS];
-    float factor = 0.f, m = 0.f, mv = 0.f, l = 0.f;
+    // One reference r for numerator and sum: the weights are 2^(score + log2(value scale) - r),
+    // and the sum takes each block's value scale back.  Value scales are relative to
+    // 2^level, that of the unit's first page here.
+    float factor = 0.f, ref = 0.f, l = 0.f, level = 0.f;
     f32x16 o[DT];
     int pos = -1, from = cur.page, low = -1, top = -1;
     bool open = true, wild = false;
@@ -701,8 +705,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void attend_ch
             for (int s = 0; s < KS; ++s)
                 for (int j = 0; j < 8; ++j) q[s][j] = (_Float16)(sign * ldexpf(y[s][j], e));
             factor = ldexpf(fabsf(a.scale2), -e);
-            m = mv = -__builtin_inff();
+            ref = -__builtin_inff();
             l = 0.f;
+            level = 0.f;
+            for (int b = 0; b < 4; ++b) level = fmaxf(level, here.vs[b]);
+            level = level > 0.f ? __builtin_amdgcn_logf(level) : 0.f;
             wild = false;
             for (int d = 0; d < DT; ++d)
                 for (int j = 0; j < 16; ++j) o[d][j] = 0.f;
@@ -745,48 +752,40 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void attend_ch
                     if (key > pos || !now.fits) s[j >> 4][j & 15] = -__builtin_inff();
                 }
             }
-            float f[4], vlog[4], top1 = -__builtin_inff(), top2 = -__builtin_inff();
+            float f[4], vlog[4], top1 = -__builtin_inff();
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 f[b] = fmaxf(factor * now.ks[b], 0x1p-126f);   // never 0: a masked score stays -inf
-                vlog[b] = now.vs[b] > 0.f ? __builtin_amdgcn_logf(now.vs[b]) : -__builtin_inff();
+                // (a block without a value scale has codes of 0 and may have any)
+                vlog[b] = now.vs[b] > 0.f ? __builtin_amdgcn_logf(now.vs[b]) - level : 0.f;
                 float big = max3(s[b >> 1][8 * (b & 1)], s[b >> 1][8 * (b & 1) + 1], s[b >> 1][8 * (b & 1) + 2]);
                 big = max3(big, s[b >> 1][8 * (b & 1) + 3], s[b >> 1][8 * (b & 1) + 4]);
                 big = max3(big, s[b >> 1][8 * (b & 1) + 5], s[b >> 1][8 * (b & 1) + 6]);
-                big = fmaxf(big, s[b >> 1][8 * (b & 1) + 7]) * f[b];
-                top1 = fmaxf(top1, big);
-                top2 = fmaxf(top2, big + vlog[b]);
+                top1 = fmaxf(top1, __builtin_fmaf(fmaxf(big, s[b >> 1][8 * (b & 1) + 7]), f[b], vlog[b]));
             }
             top1 = max_of_halves(top1);
-            top2 = max_of_halves(top2);
-            const bool over = top1 > m + kLag || top2 > mv + kLag;
+            const bool over = top1 > ref + kLag;
             if (__any(over)) {   // each row by itself, so that none depends on its neighbours
-                const float m1 = over ? fmaxf(m, top1) : m, m2 = over ? fmaxf(mv, top2) : mv;
-                l *= m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - m1);
-                const float back = mv == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(mv - m2);
+                const float r1 = over ? fmaxf(ref, top1) : ref;
+                const float back = ref == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ref - r1);
+                l *= back;
 #pragma unroll
                 for (int d = 0; d < DT; ++d) o[d] *= back;
-                m = m1;
-                mv = m2;
-                wild = __any(fabsf(m1) > 0x1p8f && m1 > -__builtin_inff());
+                ref = r1;
+                wild = __any(fabsf(ref) > 0x1p8f && ref > -__builtin_inff());
             }
-            // Weight and value scale in one exponent, 2^(s f - m) 2^gain; the sum
-            // takes the gain back, once per block.  A block without a value scale has codes of 0 and may
-            // have any; one of 2^-60 and less rounds to 0 next to the largest.
-            const float m1 = m == -__builtin_inff() ? 0.f : m, m2 = mv == -__builtin_inff() ? 0.f : mv;
-            float gain[4], shift[4];
+            float shift[4];
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                gain[b] = vlog[b] == -__builtin_inff() ? kUnit : fminf(fmaxf(vlog[b] + (m1 - m2) + kUnit, -60.f), 126.f);
-                shift[b] = gain[b] - m1;
-            }
-            if (wild) {   // a maximum whose fractions float32 rounds off: scores relative to it first
+            for (int b = 0; b < 4; ++b) shift[b] = (vlog[b] + kUnit) - (ref == -__builtin_inff() ? 0.f : ref);
+            if (wild) {   // a reference whose fractions float32 rounds off: scores relative to it first
+                const bool mine = fabsf(ref) > 0x1p8f && ref > -__builtin_inff();
 #pragma unroll
-                for (int j = 0; j < 32; ++j) s[j >> 4][j & 15] = scaled_less(s[j >> 4][j & 15], f[j >> 3], m1);
+                for (int j = 0; j < 32; ++j)
+                    if (mine) s[j >> 4][j & 15] = scaled_less(s[j >> 4][j & 15], f[j >> 3], ref);
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
-                    f[b] = 1.f;
-                    shift[b] = gain[b];
+                    f[b] = mine ? 1.f : f[b];
+                    shift[b] = mine ? vlog[b] + kUnit : shift[b];
                 }
             }
             f16x8 w[4], wl[PARTS > 1 ? 4 : 1];
@@ -800,7 +799,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void attend_ch
                     w[b][i] = (_Float16)y;
                     if constexpr (PARTS > 1) wl[b][i] = (_Float16)(y - (float)w[b][i]);
                 }
-                l += (sum[0] + sum[1]) * __builtin_amdgcn_exp2f(-gain[b]);
+                l = __builtin_fmaf(sum[0] + sum[1], __builtin_amdgcn_exp2f(-vlog[b]), l);
             }
 #pragma unroll
             for (int b = 0; b < 4; ++b)
@@ -816,8 +815,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void attend_ch
         if (cur.page + 1 == cur.pages || at + 1 == end) {
             const bool whole = from == 0 && cur.page + 1 == cur.pages;
             const int place = 2 * share + (at - x == cur.page - from ? 0 : 1);   // the share's first unit, or its last
-            const float sum = sum_of_halves(l);
-            const float back = mv == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(mv - m - kUnit);
+            // out of the units of weights (2^kUnit) and of values (2^level)
+            const float sum = sum_of_halves(l) * __builtin_amdgcn_exp2f(-kUnit);
+            const float back = __builtin_amdgcn_exp2f(level - kUnit);
             const int r = r0 + wave * 32 + n;
             if (r <= last) {
                 const int64_t to = (int64_t)(cur.first + r / a.group) * a.heads + cur.kvh * a.group + r % a.group;
@@ -834,9 +834,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void attend_ch
                     }
                 if (h == 0) {
                     if (whole) {
-                        if (a.lse) a.lse[to] = log_sum(m, sum);
+                        if (a.lse) a.lse[to] = log_sum(ref, sum);
                     } else {
-                        po[D] = m;
+                        po[D] = ref;
                         po[D + 1] = sum;
                     }
                 }

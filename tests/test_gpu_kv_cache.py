@@ -240,9 +240,10 @@ def test_attend_rows_do_not_depend_on_each_other(counts):
     g = torch.Generator(device="cuda").manual_seed(11)
     q = torch.randn(sum(counts), 4, 64, generator=g, device="cuda").to(torch.float16)
     want = cache.attend(0, q, tables, ints(lens), starts_of(counts))
-    q[:, 2] *= 30
-    out = cache.attend(0, q, tables, ints(lens), starts_of(counts))
-    assert torch.equal(out[:, [0, 1, 3]], want[:, [0, 1, 3]])
+    for _ in range(2):
+        q[:, 2] *= 100
+        out = cache.attend(0, q, tables, ints(lens), starts_of(counts))
+        assert torch.equal(out[:, [0, 1, 3]], want[:, [0, 1, 3]])
 
 
 def test_attend_many_rows():
@@ -320,6 +321,25 @@ def test_scales_of_very_different_size(kind):
     q = torch.randn(1, 3, 64, device="cuda").to(torch.float16)
     out, lse = cache.attend(0, q, tables, ints([200]), return_lse=True)
     check_attend(cache, HostCache(cache, 0), rows, [200], q, [1], out, lse)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("length,count", [(200, 1), (200, 9), (200, 60), (2500, 1), (1100, 20)])
+def test_scales_of_very_different_size_in_every_path(length, count, kind):
+    # also blocks of zeros, and a first block far above or below the rest
+    cache = tq.KVCache(1, 45, 1, 64, kind)
+    dirty(cache)
+    rows, tables = table_of([length], 40, 45, 2)
+    new = new_values([length], 1, 64, torch.bfloat16, 3)
+    r = np.random.RandomState(length)
+    size = 10.0 ** r.uniform(-9, 3, length // 16 + 1)
+    size[::5] = 0
+    size[0] = 1e-12 if count % 2 else 1e6
+    v = (new[1].float() * torch.tensor(size, device="cuda", dtype=torch.float32).repeat_interleave(16)[:length, None, None]).to(torch.bfloat16)
+    cache.append(0, new[0], v, tables, ints([length]), starts_of([length]))
+    q = torch.randn(count, 8, 64, device="cuda").to(torch.float16).to(torch.bfloat16)
+    out, lse = cache.attend(0, q, tables, ints([length]), starts_of([count]), return_lse=True)
+    check_attend(cache, HostCache(cache, 0), rows, [length], q, [count], out, lse)
 
 
 def test_bad_page_ids_are_left_out():
