@@ -63,12 +63,6 @@ __device__ inline bool finite16(unsigned short u) {
     return (u & e) != e;
 }
 
-__device__ inline float max3(float a, float b, float c) {
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
-}
-
 // Piece of a row at which piece c of key row kr lies.  The banks repeat every
 // 16 pieces (256 bytes): 16 neighbouring key rows are read at one c, four
 // value rows at four neighbouring c, and both times all 16 differ.
@@ -246,8 +240,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void prompt_ke
         float big = max3(s[0][0], s[0][1], s[0][2]);
 #pragma unroll
         for (int j = 3; j < 31; j += 2) big = max3(big, s[j >> 4][j & 15], s[(j + 1) >> 4][(j + 1) & 15]);
-        big = max_of_halves(fmaxf(big, s[1][15]));
-        const bool over = (big - m) * c2 > kLag || (m == -__builtin_inff() && big > m);
+        big = max_of_halves(larger(big, s[1][15]));
+        const bool over = ((big - m) * c2 > kLag) | ((m == -__builtin_inff()) & (big > m));
         if (__any(over)) {   // each row by itself, so that none depends on its neighbours
             const float mn = over ? fmaxf(m, big) : m, mm = mn == -__builtin_inff() ? 0.f : mn;
             const float alpha = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m - mm) * c2);

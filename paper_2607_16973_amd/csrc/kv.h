@@ -133,12 +133,17 @@ __device__ inline int slot_row(const int *starts, int rows, int64_t s, int num, 
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
+// The larger; NaN if one is.  (One instruction each, also of values the matrix
+// cores have just written: fmaxf would first quiet every operand.)
+__device__ inline float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ inline float max3(float a, float b, float c) { return larger(larger(a, b), c); }
+
 // Largest / sum over the lanes l, l ^ 16, l ^ 32, l ^ 48.
 __device__ inline float max_of_groups(float x) {
     auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    x = larger(__uint_as_float(a[0]), __uint_as_float(a[1]));
     auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    return larger(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 __device__ inline float sum_of_groups(float x) {
     auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -149,7 +154,7 @@ __device__ inline float sum_of_groups(float x) {
 // The same over l and l ^ 32.
 __device__ inline float max_of_halves(float x) {
     auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    return larger(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
 __device__ inline float sum_of_halves(float x) {
     auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);

@@ -33,12 +33,6 @@ constexpr int kLine = 1 << 30;    // pages of all units together stay below
 constexpr float kUnit = 6.f;      // weights are held in units of 2^-kUnit ...
 constexpr float kLag = 8.f;       // ... and may pass the running maximum by 2^kLag before it follows
 
-__device__ inline float max3(float a, float b, float c) {
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
-}
-
 // Rows of up to kShort pages in calls of up to kFew units have a workgroup per
 // unit: 16.6 us against 20.6 for one row of 777 tokens, 37.7 against 37.4 for
 // 64 rows of 500 to 1,500 (512 units); with 2,048 units the even shares are ahead (88 us against 70),
@@ -48,6 +42,12 @@ constexpr int kShort = 24, kFew = 512;
 // 56 (8 heads of 7 tokens, three rows of up to 61,049 tokens, d = 128) 118 us against 152
 // with four tiles of 16 rows to a wave, at 30 119 us against 138 the other way round.
 constexpr int kMany = 32;
+
+// Codes in global memory, 16 at a time.
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef const u32x4 __attribute__((address_space(1))) *codes_at;
+typedef const float __attribute__((address_space(4))) *scales_at;   // uniform, not written meanwhile
+__device__ inline codes_at global_of(const void *p) { return (codes_at)(uintptr_t)p; }
 
 // 16 codes -> 2 x 8 float16.
 template <bool FP8>
@@ -229,7 +229,7 @@ __device__ inline void page_step(Rows<D, NT> &t, Page<D> &page, int index, int l
         float big = max3(s[i][0][0], s[i][0][1], s[i][0][2]);
 #pragma unroll
         for (int j = 3; j < 15; j += 2) big = max3(big, s[i][j >> 2][j & 3], s[i][(j + 1) >> 2][(j + 1) & 3]);
-        big = fmaxf(big, s[i][3][3]) * f;
+        big = larger(big, s[i][3][3]) * f;
         const float top1 = max_of_groups(big), top2 = max_of_groups(big + vlog);
         const bool over = top1 > t.m[i] + kLag || top2 > t.mv[i] + kLag;
         if (__any(over)) {   // each row by itself, so that none depends on its neighbours
@@ -585,9 +585,11 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendArgs a) {
 // codes become float16 once per workgroup, on their way through LDS, and
 // the products are 32x32x16; the codes of the page after next are on their
 // way in registers meanwhile.  A lane's 32 scores of a page are 8 of each of its
-// four blocks, so scales are uniform values again.  Bound by the
-// vector instructions: 300 and 32 exponentials per page and wave at d = 64, against
-// 16 products.  Measured: 92 us for 4 rows of up to 256 new tokens against 2,500 to
+// four blocks, so scales are uniform values again (read through the scalar
+// cache: 16 registers fewer, 127 us against 136 for 2 rows of 400 new tokens on 16,000 with
+// float16 results, whose kernel spilled before).  Bound by the
+// vector instructions: 250 and 40 exponentials per page and wave at d = 64, against
+// 16 products.  Measured: 86 us for 4 rows of up to 256 new tokens against 2,500 to
 // 8,192 cached ones, 32 heads on 8, d = 64, e4m3 (425 TFLOP/s), and 8 us to join.  PARTS: the weights go
 // to the product in that many float16 parts (two for float16 results, whose
 // own rounding is as small as that of the weights).
@@ -613,16 +615,20 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void attend_ch
         coming.fits = in && any;
         if (!in && any && a.layer.status && threadIdx.x == 0) atomicOr(a.layer.status, TQ_KV_BAD_PAGE);
         const int64_t tile = (int64_t)(coming.fits ? id : 0) * a.layer.heads + p.kvh;
-        const uint4 *kp = reinterpret_cast<const uint4 *>(a.layer.k + tile * (kPage * D)) + threadIdx.x;
-        const uint4 *vp = reinterpret_cast<const uint4 *>(a.layer.v + tile * (kPage * D)) + threadIdx.x;
+        // (opaque, so that the lanes' part of the address stays a 32-bit offset)
+        auto kp = global_of(a.layer.k + tile * (kPage * D)), vp = global_of(a.layer.v + tile * (kPage * D));
+        asm("" : "+s"(kp), "+s"(vp));
 #pragma unroll
         for (int i = 0; i < RAW; ++i) {
-            kraw[i] = kp[i * 256];
-            vraw[i] = vp[i * 256];
+            const unsigned c = threadIdx.x + i * 256;
+            kraw[i] = __builtin_bit_cast(uint4, kp[c]);
+            vraw[i] = __builtin_bit_cast(uint4, vp[c]);
         }
+        const scales_at ks = (scales_at)(uintptr_t)(a.layer.ks + tile * 4), vs = (scales_at)(uintptr_t)(a.layer.vs + tile * 4);
+#pragma unroll
         for (int b = 0; b < 4; ++b) {
-            coming.ks[b] = a.layer.ks[tile * 4 + b];
-            coming.vs[b] = a.layer.vs[tile * 4 + b];
+            coming.ks[b] = ks[b];
+            coming.vs[b] = vs[b];
         }
         // a page that holds the row's end may hold anything past it
         const int len = min(p.len, a.limit);
@@ -761,7 +767,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void attend_ch
                 float big = max3(s[b >> 1][8 * (b & 1)], s[b >> 1][8 * (b & 1) + 1], s[b >> 1][8 * (b & 1) + 2]);
                 big = max3(big, s[b >> 1][8 * (b & 1) + 3], s[b >> 1][8 * (b & 1) + 4]);
                 big = max3(big, s[b >> 1][8 * (b & 1) + 5], s[b >> 1][8 * (b & 1) + 6]);
-                top1 = fmaxf(top1, __builtin_fmaf(fmaxf(big, s[b >> 1][8 * (b & 1) + 7]), f[b], vlog[b]));
+                top1 = larger(top1, __builtin_fmaf(larger(big, s[b >> 1][8 * (b & 1) + 7]), f[b], vlog[b]));
             }
             top1 = max_of_halves(top1);
             const bool over = top1 > ref + kLag;
