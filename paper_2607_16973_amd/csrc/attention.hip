@@ -18,10 +18,10 @@
 // bank conflicts.
 // The running maximum follows only when a score passes it by 2^kLag: until
 // then weights grow up to 2^kLag instead of the accumulators being rescaled.
-// Measured: 1.02 ms for one row of 16,384 tokens, 16 heads on 2, d = 128, bfloat16
-// (1,078 TFLOP/s of the pairs that are seen; a large library product reaches 1,241 on
-// the same card).  The matrix cores are busy half of the time and vector
-// instructions (32 exponentials, 130 others per step) the other half, at a
+// Measured: 1.00 ms for one row of 16,384 tokens, 16 heads on 2, d = 128, bfloat16
+// (1,096 TFLOP/s of the pairs that are seen; a large library product reaches 1,241 on
+// the same card).  The matrix cores are busy 56% of the cycles and vector
+// instructions (32 exponentials, 120 others per step) 52%, at a
 // clock of 2.0 GHz: taking vector instructions out (no maximum per step), raising
 // the products' priority and interleaving both by hand were all slower.  At
 // d = 64 three waves per SIMD (687 TFLOP/s for 8,001 tokens) are ahead of two (575) and of

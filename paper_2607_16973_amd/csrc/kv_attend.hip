@@ -589,8 +589,8 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendArgs a) {
 // cache: 16 registers fewer, 127 us against 136 for 2 rows of 400 new tokens on 16,000 with
 // float16 results, whose kernel spilled before).  Bound by the
 // vector instructions: 250 and 40 exponentials per page and wave at d = 64, against
-// 16 products.  Measured: 86 us for 4 rows of up to 256 new tokens against 2,500 to
-// 8,192 cached ones, 32 heads on 8, d = 64, e4m3 (425 TFLOP/s), and 8 us to join.  PARTS: the weights go
+// 16 products.  Measured, 8 us to join among them: 83 us for 4 rows of up to 256 new tokens against 2,500 to
+// 8,192 cached ones, 32 heads on 8, d = 64, e4m3 (465 TFLOP/s).  PARTS: the weights go
 // to the product in that many float16 parts (two for float16 results, whose
 // own rounding is as small as that of the weights).
 template <int D, bool FP8, int PARTS>
