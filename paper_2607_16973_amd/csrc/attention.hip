@@ -126,8 +126,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void prompt_ke
     const int full = a.causal ? (int)(slot * kRows / a.group) + keys - count : keys - 1;
     const int steps = top < 0 ? 0 : top / kKeys + 1;
 
-    // a negative scale is one of the negated queries: the largest product has the largest score
-    const float c2 = fabsf(a.scale2);
+    // a negative scale is one of the negated queries: the largest product has the largest score;
+    // never 0, so that a masked score stays -inf
+    const float c2 = fmaxf(fabsf(a.scale2), 0x1p-126f);
     const unsigned flip = a.scale2 < 0.f ? 0x80008000u : 0u;
     x8 q[KS];
 #pragma unroll

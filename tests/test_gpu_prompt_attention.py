@@ -193,3 +193,13 @@ def test_long_row_against_float64_samples():
     e = HALF[torch.bfloat16]
     assert torch.all((got - ref).abs() <= (e + 2.0 ** -12) * size + e * ref.abs())
     assert torch.all((lse[at].double().cpu() - rl).abs() <= 2.0 ** -12)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-45])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_a_scale_of_zero_weighs_all_keys_alike(d, scale):
+    counts, keys = [70, 3, 130], [75, 2, 130]
+    q, k, v = rows(counts, 4, d, torch.float16, 50), rows(keys, 2, d, torch.float16, 51), rows(keys, 2, d, torch.float16, 52)
+    for causal in (True, False):
+        out, lse = tq.attention(q, k, v, starts_of(counts), starts_of(keys), causal=causal, scale=scale, return_lse=True)
+        check(q, k, v, counts, keys, out, lse, causal, scale)
