@@ -20,6 +20,7 @@ _ref = ctypes.byref
 # the raw forms: what a call costs the host is a large part of a decoding step
 _stream_of = torch._C._cuda_getCurrentRawStream
 _current_device = torch._C._cuda_getDevice
+_capturing = torch._C._cuda_isCurrentStreamCapturing
 
 
 def _on(t, shape, dtype, index, name):
@@ -51,6 +52,8 @@ def _packed(t, shape, dtype, index, name):
     try:
         if t.shape == shape and t.dtype is dtype and t.get_device() == index:
             a, b, c = t.stride()
+            if t.requires_grad and torch.is_grad_enabled():
+                raise ValueError("%s requires a gradient, and this call has none: use torch.no_grad()" % name)
             if c == 1:
                 return RowsView(t.data_ptr(), a, b)
     except AttributeError:
@@ -277,7 +280,7 @@ class KVCache:
         table, width, length, at, rows = self._rows(tables, lens, starts, n)
         need = _attend_bytes(self.kv_heads, d, n, heads, width, rows, longest)
         if workspace is not None:
-            ws = _on(workspace, workspace.shape, torch.uint8, self._index, "workspace")
+            ws = _on(workspace, _dims(workspace, 1, "workspace"), torch.uint8, self._index, "workspace")
             need = workspace.numel()
         elif need:
             workspace = q.new_empty((need,), dtype=torch.uint8)
@@ -316,7 +319,9 @@ class KVPages:
                                 _on(refs, (pages,), _I32, index, "refs"), pages, rows, width)
         _gpu(tables, "tables")
         self.tables, self.lens, self.refs = tables, lens, refs
-        self._ws = None   # kept: calls on the same rows follow one another anyway
+        # kept for the calls of one stream, which follow one another: memory
+        # goes back in the order of the stream that it came from
+        self._ws, self._ws_stream = None, None
         self._index, self._ref = index, _ref(self._view)
 
     def _workspace(self, n: int, cache):
@@ -324,9 +329,12 @@ class KVPages:
             raise ValueError("the rows, the cache and the current device must be one GPU")
         v = self._view
         need = _pages_bytes(v.pages, v.rows, v.width, n)
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = self.lens.new_empty((need,), dtype=torch.uint8)
-        return self._ws
+        stream = _stream_of(self._index)
+        if _capturing():   # a graph's workspace is the graph's, however long this object keeps its own
+            return self.lens.new_empty((need,), dtype=torch.uint8), stream
+        if stream != self._ws_stream or self._ws.numel() < need:
+            self._ws, self._ws_stream = self.lens.new_empty((need,), dtype=torch.uint8), stream
+        return self._ws, stream
 
     def resize(self, goals, cache: KVCache) -> None:
         """Sets the rows' lengths to goals (int32 [rows], negative: leave):
@@ -334,8 +342,8 @@ class KVPages:
         pages in row order (tq_kv_resize).  A row that does not get its pages
         stays as it is, and cache.check() says so."""
         at = _on(goals, self.lens.shape, _I32, self._index, "goals")
-        ws = self._workspace(0, cache)
-        check(lib.tq_kv_resize(self._ref, at, cache._ref, ws.data_ptr(), ws.numel(), _stream_of(self._index)))
+        ws, stream = self._workspace(0, cache)
+        check(lib.tq_kv_resize(self._ref, at, cache._ref, ws.data_ptr(), ws.numel(), stream))
 
     def fork(self, src, dst, cache: KVCache) -> None:
         """Makes rows dst (int32 [n], distinct) copies of rows src (int32
@@ -343,15 +351,13 @@ class KVPages:
         layer (tq_kv_fork)."""
         shape = _dims(src, 1, "src")
         a, b = _on(src, shape, _I32, self._index, "src"), _on(dst, shape, _I32, self._index, "dst")
-        ws = self._workspace(shape[0], cache)
-        check(lib.tq_kv_fork(self._ref, a, b, shape[0], cache._ref, ws.data_ptr(), ws.numel(),
-                             _stream_of(self._index)))
+        ws, stream = self._workspace(shape[0], cache)
+        check(lib.tq_kv_fork(self._ref, a, b, shape[0], cache._ref, ws.data_ptr(), ws.numel(), stream))
 
     def compact(self, cache: KVCache):
         """Moves the live pages to the front of the pool and returns their
         number (cuda int32 [1]); the pages from there on are free (tq_kv_compact)."""
         live = self.lens.new_empty(1)
-        ws = self._workspace(0, cache)
-        check(lib.tq_kv_compact(self._ref, cache._ref, live.data_ptr(), ws.data_ptr(), ws.numel(),
-                                _stream_of(self._index)))
+        ws, stream = self._workspace(0, cache)
+        check(lib.tq_kv_compact(self._ref, cache._ref, live.data_ptr(), ws.data_ptr(), ws.numel(), stream))
         return live

@@ -175,3 +175,31 @@ def test_graph_of_a_resize():
         assert b.dev.tables.tolist() == b.host.tables and b.dev.refs.tolist() == b.host.refs
         b.host.resize([70, 80, 30])
         b.host.resize([10, 20, 0])
+
+
+def test_workspaces_of_streams_and_graphs():
+    # a workspace that work of another stream or a graph may still use is not given away
+    b = Both(6, 4, 30)
+    b.resize([100, 70, 0, 0, 0, 0])
+    main, side = b.dev._ws, torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        b.resize([130, 70, 10, 0, 0, 0])
+        assert b.dev._ws is not main and b.dev._ws_stream == side.cuda_stream
+    torch.cuda.current_stream().wait_stream(side)
+    b.resize([130, 80, 10, 0, 0, 0])
+    kept, goals = b.dev._ws, ints([0] * 6)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.dev.resize(goals, b.cache)
+    assert b.dev._ws is kept
+    b.fork([0, 1], [3, 4])
+    b.fork([0, 1, 0], [3, 4, 5])                 # a larger one: the kept one goes
+    junk = torch.full((1 << 20,), -1, dtype=torch.int32, device="cuda")
+    for step in ([200, 80, 10, 130, 80, 130], [64, 0, 10, 1, 80, 256], [7, 7, 7, 7, 7, 7]):
+        before = [t.clone() for t in b._state()]
+        copies = b.host.resize(step)
+        goals.copy_(ints(step))
+        graph.replay()
+        b._done(before, copies)
+    assert bool((junk == -1).all())
