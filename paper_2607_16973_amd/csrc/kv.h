@@ -111,6 +111,9 @@ __device__ inline void row_tokens(const int *starts, int i, int total, int *firs
     *count = min(max(starts[i + 1] - a, 0), total - a);
 }
 
+// The length of row i; negative ones count as 0, so that what is computed from it stays in range.
+__device__ inline int row_length(const int *lens, int i) { return max(lens[i], 0); }
+
 // Work slots of rows without a list made by the host: row i owns the slots
 // from f(i) = starts[i] * num / den + i * extra on; the row of slot s is the last i
 // with f(i) <= s.  (num / den slots per token, extra more per row.)

@@ -239,7 +239,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
         local = 0;
     }
     row_tokens(set.starts, row, set.total, &first, &count);
-    const int true_len = set.lens[row], len = min(true_len, set.width * kPage);
+    const int true_len = row_length(set.lens, row), len = min(true_len, set.width * kPage);
     const int begin = true_len - count;                // position of the first new token
     if (local < 0 || local > count / kBlock + 1) return;   // the whole workgroup
     const int blk = max(begin, 0) / kBlock + (int)local;

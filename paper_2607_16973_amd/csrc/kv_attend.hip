@@ -319,7 +319,7 @@ __global__ __launch_bounds__(64 * W) void attend_short_kernel(AttendArgs a) {
 
     // the row's length, the wave's first page id and the queries at once
     const int *table = a.set.tables + (int64_t)row * a.set.width;
-    const int true_len = a.set.lens[row];
+    const int true_len = row_length(a.set.lens, row);
     int ahead = wave < a.set.width ? table[wave] : -1;
     Rows<D, NT> t;
     t.load(a, r0, last, first, kvh, n, g);
@@ -404,7 +404,7 @@ struct Place {                       // a page of the line; the same in all lane
 template <int RT>
 __device__ inline void row_shape(const AttendArgs &a, int row, Place *p) {
     row_tokens(a.set.starts, row, a.set.total, &p->first, &p->count);
-    p->len = a.set.lens[row];
+    p->len = row_length(a.set.lens, row);
     p->tiles = (p->count * a.group + RT - 1) / RT;
     p->pages = max((min(p->len, a.limit) + kPage - 1) / kPage, 1);
 }
@@ -863,7 +863,8 @@ __device__ inline bool find_parts(const AttendArgs &a, int64_t at, int row, int 
     const int2 info = reinterpret_cast<const int2 *>(a.info)[unit_of<RT>(a, row, first, r / RT, head / a.group)];
     *place = info.x, *parts = info.y, *inside = r % RT;
     // (starts that do not ascend may leave a unit without an owner)
-    return info.y > 1 && info.x >= 0 && info.y <= a.shares && (info.x & ~1) + 2 * (info.y - 1) < 2 * a.shares;
+    return info.y > 1 && info.y <= a.shares && info.x >= 0 && info.x < 2 * a.shares &&
+           (info.x & ~1) + 2 * (info.y - 1) < 2 * a.shares;
 }
 // The c-th part of a unit: the first one's place, then the first unit of each following share.
 template <int D, int RT>

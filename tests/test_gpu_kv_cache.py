@@ -454,3 +454,37 @@ def test_graph_of_a_step():
         torch.cuda.synchronize()
         assert torch.equal(out, eager)
         cache.attend(0, q, tables, lens)
+
+
+@pytest.mark.parametrize("counts", [None, [2, 1], [40, 90]])
+@pytest.mark.parametrize("length", [-1, -70, -2 ** 31])
+def test_negative_lengths_are_empty_rows(length, counts):
+    cache, rows, tables = filled([30, 100], 30, 40, 2, 64, "int8")
+    lens = ints([length, 100])
+    starts = None if counts is None else starts_of(counts)
+    counts = counts or [1, 1]
+    before = HostCache(cache, 0)
+    new = new_values(counts, 2, 64, torch.float16, 31)
+    q = torch.randn(sum(counts), 4, 64, device="cuda").to(torch.float16)
+    for longest in (0, 128):                     # long rows' path and that of short ones
+        out, lse = cache.attend(0, q, tables, lens, starts, longest=longest, return_lse=True)
+        check_attend(cache, before, rows, [0, 100], q, counts, out, lse)
+    cache.append(0, new[0], new[1], tables, lens, starts)
+    after = HostCache(cache, 0)
+    for was, now in zip(before.codes + before.scales, after.codes + after.scales):
+        assert np.array_equal(was[rows[0]], now[rows[0]], equal_nan=True)
+    cache.check()
+
+
+def test_queries_that_want_gradients_are_refused():
+    cache, rows, tables = filled([30], 2, 3, 2, 64, "int8")
+    q, lens = torch.randn(1, 4, 64, device="cuda").to(torch.float16).requires_grad_(), ints([30])
+    new = new_values([1], 2, 64, torch.float16, 3)
+    with pytest.raises(ValueError, match="requires a gradient"):
+        cache.attend(0, q, tables, lens)
+    with pytest.raises(ValueError, match="requires a gradient"):
+        cache.append(0, new[0], new[1].requires_grad_(), tables, lens)
+    with pytest.raises(ValueError, match="requires a gradient"):
+        tq.attention(q, q.detach(), q.detach(), ints([0, 1]))
+    with torch.no_grad():
+        assert torch.equal(cache.attend(0, q, tables, lens), cache.attend(0, q.detach(), tables, lens))
