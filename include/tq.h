@@ -429,8 +429,8 @@ int32_t tq_last_search_fallbacks(void);
  * call's packed new tokens are whose.  NULL starts_dev: one new token per
  * row.  The i-th of a row's n new tokens has position len - n + i.
  * Values that lie on the device are not checked by the host: a page id outside [0, pages) is
- * skipped (TQ_KV_BAD_PAGE), a length beyond width pages is cut, tokens
- * outside the packed tensor are left out. */
+ * skipped (TQ_KV_BAD_PAGE), a length beyond width pages is cut, a negative one
+ * is 0, tokens outside the packed tensor are left out. */
 typedef enum { TQ_KV_INT8 = 0, TQ_KV_FP8 = 1 } tq_kv_type;
 typedef enum { TQ_F16 = 0, TQ_BF16 = 1 } tq_float;
 #define TQ_KV_PAGE 64

@@ -1,6 +1,7 @@
 """Binding of the reader's calls (include/tq.h, "a language model's reader"):
 shapes, types and devices are checked here, everything else runs in the
-library.  Nothing in this file waits for the GPU except KVCache.check()."""
+library.  The calls have no backward pass: inputs that require a gradient are
+refused unless gradients are off.  Nothing in this file waits for the GPU except KVCache.check()."""
 from __future__ import annotations
 
 import ctypes
