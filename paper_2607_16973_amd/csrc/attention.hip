@@ -37,6 +37,7 @@ namespace {
 constexpr int kKeys = 64;     // keys of a step
 constexpr int kRows = 128;    // query rows of a workgroup
 constexpr int kShortTiles = 4;
+constexpr int kParts = 4;     // see long_first
 constexpr float kLag = 8.f;   // log2 of the weight at which the maximum must follow
 
 template <bool BF16>
@@ -80,6 +81,30 @@ __device__ inline u32x2 read_transposed(uint32_t at) {
     return __builtin_bit_cast(u32x2, r);
 }
 
+// Workgroup number at of `all` (per key head) takes a tile of a row: the upper halves of all rows'
+// tiles first, then the quarters below them, and so on, so that what comes last is
+// short whichever row it is of, while neighbours still share a row's keys.  Row i's
+// tiles are its slots [end_0(i), end_0(i + 1)), and the lower 2^-p of them
+// [end_p(i), end_p(i + 1)), end_p(i) = starts[i] * group / (kRows 2^p) for p > 0: these floors
+// nest, so that every slot is in one part.
+__device__ inline int long_first(const PromptArgs &a, int64_t all, int64_t at, int64_t *tile) {
+    const auto end = [&](int i, int p) { return slot_begin(a.starts, i, a.group, kRows << p, p == 0); };
+    int p = 0;
+    int64_t above = all, below = 0;                       // slots of the lower 2^-p, and of the half of them
+    for (;; ++p) {
+        below = p + 1 < kParts ? min(max((int64_t)a.total * a.group / (kRows << (p + 1)), (int64_t)0), above) : 0;
+        if (p + 1 == kParts || at < above - below) break;
+        at -= above - below;
+        above = below;
+    }
+    const bool rest = p + 1 == kParts;
+    const int64_t s = above - below - 1 - at;
+    const int row = row_of_slot(a.rows, s, [&](int i) { return end(i, p) - (rest ? 0 : end(i, p + 1)); });
+    const int64_t under = rest ? 0 : end(row + 1, p + 1) - end(row, p + 1);
+    *tile = under + s - (end(row, p) - (rest ? 0 : end(row, p + 1)));
+    return row;
+}
+
 // WIDE: 16-byte loads are aligned, so that rows can go straight into LDS.
 // SHORT: a grid of a.levels tiles per row, where the longest row is known to have no more
 // than kShortTiles: the row needs no search.  Rows that are longer than that all the same are
@@ -104,9 +129,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void prompt_ke
         slot = a.levels - 1 - at / a.rows;
         row = at % a.rows;
     } else {
-        slot = (int64_t)(gridDim.x - 1 - blockIdx.x) / a.kv_heads;
-        row = slot_row(a.starts, a.rows, slot, a.group, kRows, 1);
-        slot -= slot_begin(a.starts, row, a.group, kRows, 1);
+        row = long_first(a, gridDim.x / a.kv_heads, blockIdx.x / a.kv_heads, &slot);
     }
     int first, count, kfirst, keys;
     row_tokens(a.starts, row, a.total, &first, &count);

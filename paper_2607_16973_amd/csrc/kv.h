@@ -120,20 +120,24 @@ __device__ inline int row_length(const int *lens, int i) { return max(lens[i], 0
 __device__ inline int64_t slot_begin(const int *starts, int i, int num, int den, int extra) {
     return (int64_t)starts[i] * num / den + (int64_t)i * extra;
 }
-// Called by whole waves: the 64 lanes look at 64 places at once, so up to 64
-// rows take one round of loads, up to 4,096 two.
-__device__ inline int slot_row(const int *starts, int rows, int64_t s, int num, int den, int extra) {
+// The last row i with begin(i) <= s, begin ascending.  Called by whole waves: the 64 lanes
+// look at 64 places at once, so up to 64 rows take one round of loads, up to 4,096 two.
+template <class F>
+__device__ inline int row_of_slot(int rows, int64_t s, F begin) {
     const int lane = __lane_id();
     int lo = 0, n = rows;
     while (n > 1) {
         const int step = (n + 63) >> 6, i = lane * step;
-        const bool le = i < n && slot_begin(starts, lo + i, num, den, extra) <= s;
+        const bool le = i < n && begin(lo + i) <= s;
         const int past = __popcll(__ballot(le));
         if (past == 0) break;
         lo += (past - 1) * step;
         n = min(step, n - (past - 1) * step);
     }
     return __builtin_amdgcn_readfirstlane(lo);
+}
+__device__ inline int slot_row(const int *starts, int rows, int64_t s, int num, int den, int extra) {
+    return row_of_slot(rows, s, [=](int i) { return slot_begin(starts, i, num, den, extra); });
 }
 
 // The larger; NaN if one is.  (One instruction each, also of values the matrix
