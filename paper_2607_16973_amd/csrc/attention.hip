@@ -86,7 +86,8 @@ __device__ inline u32x2 read_transposed(uint32_t at) {
 // short whichever row it is of, while neighbours still share a row's keys.  Row i's
 // tiles are its slots [end_0(i), end_0(i + 1)), and the lower 2^-p of them
 // [end_p(i), end_p(i + 1)), end_p(i) = starts[i] * group / (kRows 2^p) for p > 0: these floors
-// nest, so that every slot is in one part.
+// nest, so that every slot is in one part.  Eight rows of 130 to 2,048 tokens, 32 heads on 8,
+// d = 128: 135 us against 143 with one row after the other; seven parts measured the same as four.
 __device__ inline int long_first(const PromptArgs &a, int64_t all, int64_t at, int64_t *tile) {
     const auto end = [&](int i, int p) { return slot_begin(a.starts, i, a.group, kRows << p, p == 0); };
     int p = 0;

@@ -203,3 +203,18 @@ def test_a_scale_of_zero_weighs_all_keys_alike(d, scale):
     for causal in (True, False):
         out, lse = tq.attention(q, k, v, starts_of(counts), starts_of(keys), causal=causal, scale=scale, return_lse=True)
         check(q, k, v, counts, keys, out, lse, causal, scale)
+
+
+@pytest.mark.parametrize("heads,kv_heads,most", [(4, 2, 3000), (40, 1, 300), (3, 3, 1500)])
+def test_rows_of_any_lengths_as_each_alone(heads, kv_heads, most):
+    # every tile of every row is somebody's, in whatever order they are taken
+    r = np.random.RandomState(heads)
+    counts = [int(n) for n in most * r.rand(90) ** 4]
+    counts[5], counts[40], counts[-1] = most, 0, most // 2
+    q, k, v = (rows(counts, h, 64, torch.bfloat16, s) for h, s in ((heads, 61), (kv_heads, 62), (kv_heads, 63)))
+    out, lse = tq.attention(q, k, v, starts_of(counts), return_lse=True)
+    t = 0
+    for n in counts:
+        one, one_lse = tq.attention(q[t:t + n], k[t:t + n], v[t:t + n], starts_of([n]), return_lse=True)
+        assert torch.equal(out[t:t + n], one) and torch.equal(lse[t:t + n], one_lse)
+        t += n
