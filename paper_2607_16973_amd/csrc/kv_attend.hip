@@ -790,8 +790,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? 3 : 2) void attend_ch
                     if (mine) s[j >> 4][j & 15] = scaled_less(s[j >> 4][j & 15], f[j >> 3], ref);
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
+                    // One key may have all the weight here: its weight of 2^(value scale) is
+                    // made a float16, so that product and sum have the same (a change of the
+                    // block's weights by 2^-12 at most)
+                    const float unit = (float)(_Float16)__builtin_amdgcn_exp2f(vlog[b] + kUnit);
+                    const bool normal = unit >= 0x1p-14f && unit <= 65504.f;
                     f[b] = mine ? 1.f : f[b];
-                    shift[b] = mine ? vlog[b] + kUnit : shift[b];
+                    shift[b] = mine ? normal ? __builtin_amdgcn_logf(unit) : vlog[b] + kUnit : shift[b];
                 }
             }
             f16x8 w[4], wl[PARTS > 1 ? 4 : 1];

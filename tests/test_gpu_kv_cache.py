@@ -488,3 +488,21 @@ def test_queries_that_want_gradients_are_refused():
         tq.attention(q, q.detach(), q.detach(), ints([0, 1]))
     with torch.no_grad():
         assert torch.equal(cache.attend(0, q, tables, lens), cache.attend(0, q.detach(), tables, lens))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_a_key_with_all_the_weight_gives_its_values(kind):
+    # every key in turn, in the chunked kernel: its values, rounded once.  Weights of
+    # 2^-12 next to the sum's would show where a value lies near the middle between two bfloat16.
+    n, d = 200, 64
+    cache, rows, tables = filled([n], 4, 8, 1, d, kind, seed=3)
+    k, v = HostCache(cache, 0).row(rows[0], n)
+    q = (k[:, 0] * 1e18).to(torch.bfloat16).cuda()[:, None].repeat(1, 2, 1)
+    x = q[:, 0].double().cpu() @ k[:, 0].T
+    x.masked_fill_(torch.arange(n)[None, :] > torch.arange(n)[:, None], -math.inf)
+    best = x.topk(2).values
+    sure = best[:, 0] - best[:, 1] > 1e-5 * best[:, 0].abs()
+    assert sure.sum() > n // 2
+    out = cache.attend(0, q, tables, ints([n]), starts_of([n]))
+    got, want = out[:, 0].double().cpu()[sure], v[x.argmax(1), 0][sure]
+    assert torch.all((got - want).abs() <= (2.0 ** -8 + 2.0 ** -18) * want.abs())
